@@ -29,6 +29,12 @@
  *                        the batch products on FP8 E4M3 codes, the
  *                        batch-free steps in fp32; comera_fp8_quantize is
  *                        its quantiser.
+ *   comera_dense_embed_forward / _backward   an uncompressed embedding table
+ *                        with a scale, and its gradient by sorted tokens.
+ *   comera_block_norm_forward / _backward    the norms before and after a
+ *                        block with its gate and residual scale.
+ *   comera_grad_norm, comera_grad_clip       the global norm of a step's
+ *                        gradients, and their clipping.
  *
  * Conventions shared by every call:
  *   - X, Y, dY, dX are row-major [b, N] in the activation dtype of the plan
@@ -337,6 +343,150 @@ comera_status comera_tt_embed_backward_ex(const comera_tt_embed_shape *s, const 
                                           const float *const *G, const float *const *D,
                                           float *const *dG, int32_t flags, void *ws,
                                           size_t ws_bytes, int32_t *err_flag, void *stream);
+
+/* ---------------------------------------------------------------------
+ * Around the compressed layers of a training step.  Beside the conventions
+ * above, the calls below run on the current device, which must be the one of
+ * `stream` and of every buffer; buffers need the alignment of their entries
+ * only (workspaces 8 bytes).  A workspace carries nothing from one call to
+ * the next, and calls that may overlap need one each. */
+
+/* An uncompressed embedding table T[V, E], row-major. */
+typedef struct {
+    int64_t V, E;                         /* rows and width, >= 1 */
+    int32_t table;                        /* comera_dtype of T, or of dT */
+    int32_t act;                          /* comera_dtype of Y, dY */
+} comera_dense_embed_shape;
+
+/* Workspace bytes of comera_dense_embed_backward (0 for a shape or a number
+ * of tokens that is refused). */
+size_t comera_dense_embed_workspace_bytes(const comera_dense_embed_shape *s, int64_t n_tokens);
+
+/* Y[t, :] = scale * T[ids[t], :] for t < n_tokens, formed in fp32 and
+ * rounded once.
+ *   ids       device int64 [n_tokens].
+ *   Y         device [n_tokens, E].
+ *   err_flag  device int32 or NULL: set to 1 if some id is outside [0, V)
+ *             (those rows are written as zeros); never cleared by the call.
+ * n_tokens == 0: nothing is done.  Errors: bad shape, dtype, pointer or
+ * number of tokens, a scale that is not finite -> INVALID_ARG; V or E of
+ * 2^31 - 1 and more -> UNSUPPORTED. */
+comera_status comera_dense_embed_forward(const comera_dense_embed_shape *s, const int64_t *ids, int64_t n_tokens,
+                                         const void *T, float scale, void *Y, int32_t *err_flag, void *stream);
+
+/* dT[v, :] = scale * sum over the tokens t with ids[t] = v of dY[t, :], in
+ * the dtype `table` of the shape; rows without tokens are zeros (all of dT is
+ * written, also for n_tokens == 0).  Tokens are grouped by id and summed in
+ * fp32 in a fixed order: bitwise reproducible.
+ *   pad_id    tokens with this id give nothing; -1 for none.
+ *   err_flag  as for the forward; ids outside [0, V) give nothing.
+ * Errors as for the forward; pad_id outside [-1, V) -> INVALID_ARG; a missing
+ * or short workspace -> WORKSPACE. */
+comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, const int64_t *ids, int64_t n_tokens,
+                                          const void *dY, float scale, int64_t pad_id, void *dT, void *ws,
+                                          size_t ws_bytes, int32_t *err_flag, void *stream);
+
+#define COMERA_NORM_NONE 0
+#define COMERA_NORM_RMS 1     /* v / sqrt(mean(v^2) + eps) */
+#define COMERA_NORM_LAYER 2   /* (v - mean(v)) / sqrt(var(v) + eps) */
+#define COMERA_GATE_NONE 0
+#define COMERA_GATE_CHANNEL 1 /* gate fp32 [width], a parameter */
+#define COMERA_GATE_TOKEN 2   /* gate [b, width], an activation */
+
+/* What stands between two blocks of a transformer, the first with output F
+ * and the second with input H, on a residual stream X:
+ *   Xn = res_scale * X + branch_scale * gate * Npost(F)
+ *   H  = Npre(Xn)
+ * A norm's row is multiplied by its weight and its bias is added (fp32
+ * [width]; NULL: ones and zeros). */
+typedef struct {
+    int64_t width;                        /* 1 .. 8192; wider rows are UNSUPPORTED */
+    int32_t stream;                       /* comera_dtype of X, Xn, dX, dXn */
+    int32_t act;                          /* comera_dtype of F, H, dF, dH and a token gate; an fp32 act with a
+                                             bf16 stream is UNSUPPORTED */
+    int32_t post, pre;                    /* COMERA_NORM_* */
+    int32_t gate;                         /* COMERA_GATE_* */
+    float eps;                            /* > 0 */
+    float res_scale, branch_scale;
+} comera_block_norm_shape;
+
+/* Workspace bytes of comera_block_norm_backward for b rows (0 for a shape
+ * that is refused). */
+size_t comera_block_norm_workspace_bytes(const comera_block_norm_shape *s, int64_t b);
+
+/* Xn [b, width] and H [b, width] from X and F [b, width], rows contiguous;
+ * sums in fp32, each output rounded once (H is taken from Xn before its
+ * rounding).
+ *   F       NULL: there is no block before (the first pre-norm of a stack).
+ *           Xn is X then and is not written: H = Npre(X); gate and post-norm
+ *           are not passed.
+ *   Xn      NULL: not written (the last norm of a stack).
+ *   H       NULL if and only if pre is COMERA_NORM_NONE.
+ *   gate    as the shape's gate says; NULL for COMERA_GATE_NONE.
+ * Xn may be X, and H may be F, of the same dtype; otherwise outputs do not
+ * overlap inputs.  b == 0: nothing is done.  A pointer that the shape rules
+ * out, or a missing one, is INVALID_ARG. */
+comera_status comera_block_norm_forward(const comera_block_norm_shape *s, int64_t b, const void *X, const void *F,
+                                        const float *post_w, const float *post_b, const void *gate, const float *pre_w,
+                                        const float *pre_b, void *Xn, void *H, void *stream);
+
+/* Gradients from dXn and dH (either may be NULL: zero), with Xn as the
+ * forward call wrote it (X itself where F is NULL):
+ *   T = dXn + Npre'(dH);  dX = res_scale T (dX = T where F is NULL)
+ *   dF = Npost'(branch_scale gate T);  dgate = branch_scale T Npost(F)
+ * and the sums over the rows for the weights and biases (dgate of
+ * COMERA_GATE_CHANNEL among them: fp32 [width]; of COMERA_GATE_TOKEN it is
+ * [b, width] in act).  Xn may be NULL where dH is.  Outputs may be NULL: not
+ * computed.  dX may be dXn, dF may be F or dH and dgate of a token gate may
+ * be gate; otherwise outputs do not overlap inputs.  Sums run in fp32 in a
+ * fixed order (bitwise repeatable); b == 0 writes zeros to the parameters'
+ * gradients.  ws is needed where a parameter's gradient is asked for. */
+comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64_t b, const void *Xn, const void *F,
+                                         const float *post_w, const float *post_b, const void *gate,
+                                         const float *pre_w, const void *dXn, const void *dH, void *dX, void *dF,
+                                         void *dgate, float *dpost_w, float *dpost_b, float *dpre_w, float *dpre_b,
+                                         void *ws, size_t ws_bytes, void *stream);
+
+/* One gradient tensor of n contiguous entries. */
+typedef struct {
+    const void *g;                        /* device */
+    void *out;                            /* device, receives the clipped gradient; NULL or g: in place */
+    int64_t n;                            /* 0: the tensor is passed over */
+    int32_t dtype;                        /* comera_dtype of g and out */
+    int32_t pad_;
+} comera_grad_tensor;
+
+typedef struct comera_grad_plan_s *comera_grad_plan_t;
+
+/* Lays out a list of gradient tensors (cores, rank masks, embedding tables,
+ * norm weights: any number and size) for the two calls below.  Host only; the
+ * plan holds the addresses, which have to stay valid while it is used, and is
+ * never changed, so it may be used from several streams if each has its own
+ * workspace.  No two buffers of the list may overlap (INVALID_ARG), nor be
+ * misaligned for their dtype.  Release with comera_grad_plan_destroy. */
+comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count, comera_grad_plan_t *out);
+void comera_grad_plan_destroy(comera_grad_plan_t p);
+
+/* Device workspace (bytes) of either call; 0 for a NULL plan. */
+size_t comera_grad_workspace_bytes(comera_grad_plan_t p);
+
+/* norm = scale * sqrt(sum of the squares of all entries of all tensors), in
+ * 64 bits and a fixed order; scale > 0 (the inverse of a loss scale, or of
+ * the number of accumulated batches).
+ *   norm    device fp32 or NULL.
+ *   flag    device int32 or NULL: set to 1 if the norm is not finite as an
+ *           fp32 value; never cleared by the call.  (One of the two at least
+ *           for comera_grad_norm.) */
+comera_status comera_grad_norm(comera_grad_plan_t p, float scale, float *norm, int32_t *flag, void *ws,
+                               size_t ws_bytes, void *stream);
+
+/* The same norm (before clipping), and every tensor's
+ *   out = scale * min(1, max_norm / norm) * g
+ * with max_norm >= 0 (infinity: no clipping).  A norm that is not finite
+ * leaves the clipping out: out = scale * g, and *flag tells the caller to
+ * pass the step over. */
+comera_status comera_grad_clip(comera_grad_plan_t p, float scale, float max_norm, float *norm, int32_t *flag, void *ws,
+                               size_t ws_bytes, void *stream);
 
 /* Diagnostics for host-side tests, usable without a GPU: launch check
  * mode.  While enabled, every compute call of this library runs its whole

@@ -30,9 +30,15 @@ EXPORTS = (
     "comera_ttm_backward_masks", "comera_tt_embed_backward_ex", "comera_ttm_plan_set_fp8", "comera_fp8_quantize",
     "comera_ttm_regularizer_grads", "comera_debug_launch_check", "comera_debug_launch_count",
     "comera_debug_launch_info", "comera_ttm_forward_noalloc",
+    "comera_dense_embed_workspace_bytes", "comera_dense_embed_forward", "comera_dense_embed_backward",
+    "comera_block_norm_workspace_bytes", "comera_block_norm_forward", "comera_block_norm_backward",
+    "comera_grad_plan", "comera_grad_plan_destroy", "comera_grad_workspace_bytes", "comera_grad_norm",
+    "comera_grad_clip",
 )
 FP8_QUANTIZE_WS_BYTES = 2048
 KERNEL_FWD, KERNEL_DX, KERNEL_DW = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN = 0, 1, 2
 
 
 class ComeraError(RuntimeError):
@@ -52,6 +58,21 @@ class comera_tt_embed_shape(ctypes.Structure):
     _fields_ = [("d", ctypes.c_int32), ("pad_", ctypes.c_int32),
                 ("v", ctypes.c_int64 * MAX_CORES), ("e", ctypes.c_int64 * MAX_CORES),
                 ("r", ctypes.c_int64 * (MAX_CORES + 1))]
+
+
+class comera_dense_embed_shape(ctypes.Structure):
+    _fields_ = [("V", ctypes.c_int64), ("E", ctypes.c_int64), ("table", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+
+class comera_block_norm_shape(ctypes.Structure):
+    _fields_ = [("width", ctypes.c_int64), ("stream", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("post", ctypes.c_int32), ("pre", ctypes.c_int32), ("gate", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("res_scale", ctypes.c_float), ("branch_scale", ctypes.c_float)]
+
+
+class comera_grad_tensor(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("pad_", ctypes.c_int32)]
 
 
 _lib = None
@@ -118,6 +139,29 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.comera_ttm_plan_set_timing.restype = i32
     lib.comera_ttm_plan_kernel_time.argtypes = [vp, i32, P(dbl), P(i32)]
     lib.comera_ttm_plan_kernel_time.restype = i32
+    f32 = ctypes.c_float
+    lib.comera_dense_embed_workspace_bytes.argtypes = [P(comera_dense_embed_shape), i64]
+    lib.comera_dense_embed_workspace_bytes.restype = sz
+    lib.comera_dense_embed_forward.argtypes = [P(comera_dense_embed_shape), vp, i64, vp, f32, vp, vp, vp]
+    lib.comera_dense_embed_forward.restype = i32
+    lib.comera_dense_embed_backward.argtypes = [P(comera_dense_embed_shape), vp, i64, vp, f32, i64, vp, vp, sz, vp, vp]
+    lib.comera_dense_embed_backward.restype = i32
+    lib.comera_block_norm_workspace_bytes.argtypes = [P(comera_block_norm_shape), i64]
+    lib.comera_block_norm_workspace_bytes.restype = sz
+    lib.comera_block_norm_forward.argtypes = [P(comera_block_norm_shape), i64] + [vp] * 10
+    lib.comera_block_norm_forward.restype = i32
+    lib.comera_block_norm_backward.argtypes = [P(comera_block_norm_shape), i64] + [vp] * 16 + [sz, vp]
+    lib.comera_block_norm_backward.restype = i32
+    lib.comera_grad_plan.argtypes = [vp, i64, P(vp)]
+    lib.comera_grad_plan.restype = i32
+    lib.comera_grad_plan_destroy.argtypes = [vp]
+    lib.comera_grad_plan_destroy.restype = None
+    lib.comera_grad_workspace_bytes.argtypes = [vp]
+    lib.comera_grad_workspace_bytes.restype = sz
+    lib.comera_grad_norm.argtypes = [vp, f32, vp, vp, vp, sz, vp]
+    lib.comera_grad_norm.restype = i32
+    lib.comera_grad_clip.argtypes = [vp, f32, f32, vp, vp, vp, sz, vp]
+    lib.comera_grad_clip.restype = i32
     lib.comera_status_string.argtypes = [i32]
     lib.comera_status_string.restype = ctypes.c_char_p
     lib.comera_last_hip_error.argtypes = []
@@ -193,6 +237,49 @@ def tt_embed_shape(v: Sequence[int], e: Sequence[int], r: Sequence[int]) -> come
     for k in range(len(r)):
         s.r[k] = int(r[k])
     return s
+
+
+def dense_embed_shape(V: int, E: int, table: int = F32, act: int = F32) -> comera_dense_embed_shape:
+    return comera_dense_embed_shape(int(V), int(E), int(table), int(act))
+
+
+def block_norm_shape(width: int, stream: int = F32, act: int = F32, post: int = NORM_NONE, pre: int = NORM_RMS,
+                     gate: int = GATE_NONE, eps: float = 1e-6, res_scale: float = 1.0,
+                     branch_scale: float = 1.0) -> comera_block_norm_shape:
+    return comera_block_norm_shape(int(width), int(stream), int(act), int(post), int(pre), int(gate), float(eps),
+                                   float(res_scale), float(branch_scale))
+
+
+# ------------------------------------------------------------------ tensor checks
+# The calls around the compressed layers check the tensors that they are
+# given (raw addresses are taken as they are): a tensor of another type, a
+# strided view, one that is too short or lies on another device than the
+# current one would be read wrongly or out of its bounds.
+def _dtype_of(code: int):
+    import torch
+    return torch.bfloat16 if code == BF16 else torch.float32
+
+
+def _checked(where: str, *args) -> None:
+    """args: (tensor, torch dtype or None for any, entries) triples; None and raw addresses pass."""
+    import torch
+    dev = -1
+    for t, dtype, n in args:
+        if t is None or isinstance(t, int):
+            continue
+        at = t.get_device()
+        if at < 0:
+            raise ComeraError(ERR_INVALID_ARG, f"{where}: a tensor in host memory")
+        if dev < 0:
+            dev = torch.cuda.current_device()
+        if at != dev:
+            raise ComeraError(ERR_INVALID_ARG, f"{where}: a tensor on device {at}, the current device is {dev}")
+        if dtype is not None and t.dtype is not dtype:
+            raise ComeraError(ERR_INVALID_ARG, f"{where}: {t.dtype} where {dtype} is expected")
+        if not t.is_contiguous():
+            raise ComeraError(ERR_INVALID_ARG, f"{where}: a tensor that is not contiguous")
+        if t.numel() < n:
+            raise ComeraError(ERR_INVALID_ARG, f"{where}: {t.numel()} entries where {n} are expected")
 
 
 # ------------------------------------------------------------------ entry points
@@ -367,6 +454,146 @@ def comera_tt_embed_backward_ex(shape, ids, n_tokens: int, dY, G, D, dG, flags: 
                                             _ptr(err_flag), _stream(stream))
     _check(st, "comera_tt_embed_backward_ex")
     return st
+
+
+def comera_dense_embed_workspace_bytes(shape: comera_dense_embed_shape, n_tokens: int) -> int:
+    return int(load().comera_dense_embed_workspace_bytes(ctypes.byref(shape), int(n_tokens)))
+
+
+def comera_dense_embed_forward(shape, ids, n_tokens: int, T, scale: float, Y, err_flag=None, stream=None) -> int:
+    """Y[t, :] = scale * T[ids[t], :]."""
+    import torch
+    where = "comera_dense_embed_forward"
+    _checked(where, (ids, torch.int64, n_tokens), (T, _dtype_of(shape.table), shape.V * shape.E),
+             (Y, _dtype_of(shape.act), n_tokens * shape.E), (err_flag, torch.int32, 1))
+    st = load().comera_dense_embed_forward(shape, _ptr(ids), n_tokens, _ptr(T), scale, _ptr(Y), _ptr(err_flag),
+                                           _stream(stream))
+    _check(st, where)
+    return st
+
+
+def comera_dense_embed_backward(shape, ids, n_tokens: int, dY, scale: float, pad_id: int, dT, ws, err_flag=None,
+                                stream=None) -> int:
+    """dT[v, :] = scale * the sum of dY's rows of the tokens v; pad_id = -1 for none."""
+    import torch
+    where = "comera_dense_embed_backward"
+    _checked(where, (ids, torch.int64, n_tokens), (dY, _dtype_of(shape.act), n_tokens * shape.E),
+             (dT, _dtype_of(shape.table), shape.V * shape.E), (ws, None, 0), (err_flag, torch.int32, 1))
+    st = load().comera_dense_embed_backward(shape, _ptr(ids), n_tokens, _ptr(dY), scale, pad_id, _ptr(dT), _ptr(ws),
+                                            _nbytes(ws), _ptr(err_flag), _stream(stream))
+    _check(st, where)
+    return st
+
+
+def comera_block_norm_workspace_bytes(shape: comera_block_norm_shape, b: int) -> int:
+    return int(load().comera_block_norm_workspace_bytes(ctypes.byref(shape), int(b)))
+
+
+def comera_block_norm_forward(shape, b: int, X, F, post_w, post_b, gate, pre_w, pre_b, Xn, H, stream=None) -> int:
+    """Xn = res_scale X + branch_scale gate Npost(F), H = Npre(Xn)."""
+    import torch
+    where = "comera_block_norm_forward"
+    w, f32 = shape.width, torch.float32
+    st, act, e = _dtype_of(shape.stream), _dtype_of(shape.act), b * w
+    _checked(where, (X, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w),
+             (gate, act, e) if shape.gate == GATE_TOKEN else (gate, f32, w), (pre_w, f32, w), (pre_b, f32, w),
+             (Xn, st, e), (H, act, e))
+    rc = load().comera_block_norm_forward(shape, b, _ptr(X), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
+                                          _ptr(pre_w), _ptr(pre_b), _ptr(Xn), _ptr(H), _stream(stream))
+    _check(rc, where)
+    return rc
+
+
+def comera_block_norm_backward(shape, b: int, Xn, F, post_w, post_b, gate, pre_w, dXn, dH, dX, dF, dgate, dpost_w,
+                               dpost_b, dpre_w, dpre_b, ws, stream=None) -> int:
+    """Gradients of comera_block_norm_forward; None for an output that is not wanted."""
+    import torch
+    where = "comera_block_norm_backward"
+    w, f32 = shape.width, torch.float32
+    st, act, e = _dtype_of(shape.stream), _dtype_of(shape.act), b * w
+    gk = (act, e) if shape.gate == GATE_TOKEN else (f32, w)
+    _checked(where, (Xn, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w), (gate,) + gk, (pre_w, f32, w),
+             (dXn, st, e), (dH, act, e), (dX, st, e), (dF, act, e), (dgate,) + gk, (dpost_w, f32, w),
+             (dpost_b, f32, w), (dpre_w, f32, w), (dpre_b, f32, w), (ws, None, 0))
+    rc = load().comera_block_norm_backward(shape, b, _ptr(Xn), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
+                                           _ptr(pre_w), _ptr(dXn), _ptr(dH), _ptr(dX), _ptr(dF), _ptr(dgate),
+                                           _ptr(dpost_w), _ptr(dpost_b), _ptr(dpre_w), _ptr(dpre_b), _ptr(ws),
+                                           _nbytes(ws), _stream(stream))
+    _check(rc, where)
+    return rc
+
+
+def comera_grad_plan(tensors, count: int, raise_on_error: bool = True):
+    """Plan handle (int) for a host array of comera_grad_tensor or, with
+    raise_on_error=False, (status, handle)."""
+    h = ctypes.c_void_p()
+    st = load().comera_grad_plan(tensors, int(count), ctypes.byref(h))
+    if not raise_on_error:
+        return st, h.value
+    _check(st, "comera_grad_plan")
+    return h.value
+
+
+def comera_grad_plan_destroy(plan) -> None:
+    if plan:
+        load().comera_grad_plan_destroy(plan)
+
+
+def comera_grad_workspace_bytes(plan) -> int:
+    return int(load().comera_grad_workspace_bytes(plan))
+
+
+def comera_grad_norm(plan, scale: float, norm, flag, ws, stream=None) -> int:
+    """norm = scale * sqrt(sum of all squares); flag = 1 if it is not finite."""
+    import torch
+    _checked("comera_grad_norm", (norm, torch.float32, 1), (flag, torch.int32, 1), (ws, None, 0))
+    st = load().comera_grad_norm(plan, scale, _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws), _stream(stream))
+    _check(st, "comera_grad_norm")
+    return st
+
+
+def comera_grad_clip(plan, scale: float, max_norm: float, norm, flag, ws, stream=None) -> int:
+    """The norm, and out = scale * min(1, max_norm / norm) * g for every tensor of the plan."""
+    import torch
+    _checked("comera_grad_clip", (norm, torch.float32, 1), (flag, torch.int32, 1), (ws, None, 0))
+    st = load().comera_grad_clip(plan, scale, max_norm, _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws),
+                                 _stream(stream))
+    _check(st, "comera_grad_clip")
+    return st
+
+
+class GradPlan:
+    """Owns the plan of a list of gradient tensors, and keeps the tensors
+    alive.  outs: where the clipped gradients go (None, or a None entry: in
+    place)."""
+
+    def __init__(self, grads, outs=None):
+        self.handle = None
+        self.grads = list(grads)
+        self.outs = [None] * len(self.grads) if outs is None else list(outs)
+        if len(self.outs) != len(self.grads):
+            raise ComeraError(ERR_INVALID_ARG, "GradPlan: as many outs as grads are expected")
+        arr = (comera_grad_tensor * max(1, len(self.grads)))()
+        for i, (g, o) in enumerate(zip(self.grads, self.outs)):
+            code = {"torch.float32": F32, "torch.bfloat16": BF16}.get(str(g.dtype))
+            if code is None:
+                raise ComeraError(ERR_INVALID_ARG, f"GradPlan: {g.dtype} gradients are not taken")
+            if o is not None and o.numel() != g.numel():
+                raise ComeraError(ERR_INVALID_ARG, "GradPlan: an out of another size than its gradient")
+            _checked("GradPlan", (g, g.dtype, 0), (o, g.dtype, 0))
+            arr[i] = comera_grad_tensor(_ptr(g), _ptr(o), g.numel(), code, 0)
+        self.handle = comera_grad_plan(arr, len(self.grads))
+
+    @property
+    def workspace_bytes(self) -> int:
+        return comera_grad_workspace_bytes(self.handle)
+
+    def __del__(self):
+        try:
+            comera_grad_plan_destroy(self.handle)
+        except Exception:
+            pass
+        self.handle = None
 
 
 class TTMPlan:

@@ -1,0 +1,570 @@
+// Norms before and after a block, with its gate and residual scale:
+//   z  = Npost(F)                     (z = F without a post-norm)
+//   Xn = a X + beta * gate * z
+//   H  = Npre(Xn)
+// RMS:   N(v)_c = v_c r w_c + bias_c,           r = 1 / sqrt(mean(v^2) + eps)
+// LAYER: N(v)_c = (v_c - mean) r w_c + bias_c,  r = 1 / sqrt(var + eps)
+//
+// Backward, with y the normalised row (before w and bias) and u = dN * w:
+//   RMS   dv = r (u - y mean(u y))
+//   LAYER dv = r (u - mean(u) - y mean(u y))
+//   T = dXn + Npre'(dH);  dX = a T;  dgate = beta T z;  dF = Npost'(beta gate T)
+//   dpost_w = sum_t beta gate T y_F,  dpost_b = sum_t beta gate T,
+//   dpre_w = sum_t dH y_X,            dpre_b = sum_t dH
+// The statistics are taken again from Xn and F, whose rows the backward reads
+// in any case, so nothing is saved between the two calls.
+//
+// A row is held in the registers of LPR lanes (a wave, or several waves of
+// one workgroup), CH chunks of VEC entries a lane: every input is read once
+// and every output written once.  Bound by HBM: 4 rows forward, 6 backward.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "internal.h"
+#include "rowops.h"
+
+namespace comera {
+namespace {
+
+constexpr int kMaxWidth = 8192;
+constexpr int kMaxParts = 256;         // backward workgroups: one per CU
+constexpr int kWaveRows = 4;           // rows side by side in a workgroup when a row is one wave's
+
+struct NormArgs {
+    const void *X, *F, *gate;          // X: the residual stream (forward), Xn (backward)
+    const float *gate_ch, *post_w, *post_b, *pre_w, *pre_b;
+    const void *dXn, *dH;
+    void *Xn, *H;                      // forward
+    void *dX, *dF, *dgate;             // backward (dgate of a per-token gate)
+    float *part;                       // [workgroup][sums][N]
+    int64_t b;
+    int N, lpr, post, pre;
+    float eps, a, beta;
+};
+
+// Sums of NV values over the lanes of a row: over a wave by exchanges; rows
+// of several waves add the waves' sums in order through one of two LDS
+// buffers in turn (a buffer is written again only after a barrier that every
+// reader of its last use has passed).
+template <int NV>
+__device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[8][4], int &turn, int waves) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = wave_sum(v[i]);
+    if (waves == 1) return;
+    static_assert(NV <= 4, "four sums at most");
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) red[turn][w][i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float s = red[turn][0][i];
+        for (int x = 1; x < waves; ++x) s += red[turn][x][i];
+        v[i] = s;
+    }
+    turn ^= 1;
+}
+
+// columns of a lane: chunk j starts at col[j]; the last chunk of a row whose
+// width is no multiple of VEC is moved back to the row's end, and its first
+// skip entries, which the chunk before also holds, are left out of sums.
+// Lanes behind the row's end hold nothing (on = false).
+template <int VEC, int CH>
+struct Columns {
+    int col[CH], skip[CH];
+    bool on[CH];
+    __device__ __forceinline__ Columns(int lane, int lpr, int N) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int c = (j * lpr + lane) * VEC;
+            on[j] = c < N;
+            col[j] = on[j] ? min(c, N - VEC) : 0;
+            skip[j] = on[j] ? c - col[j] : VEC;
+        }
+    }
+    // whether entry e of chunk j counts in sums
+    __device__ __forceinline__ bool counts(int j, int e) const { return e >= skip[j]; }
+};
+
+template <class T, int VEC, int CH>
+__device__ __forceinline__ void load_row(const void *p, int64_t at, const Columns<VEC, CH> &k, float (&v)[CH * VEC]) {
+    const T *row = static_cast<const T *>(p) + at;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        Pack<T, VEC> x;
+        x.load(row + k.col[j]);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[j * VEC + e] = x.get(e);
+    }
+}
+
+// Every entry is stored by one lane alone, so an output may be the buffer of
+// an input: what another lane of the row reads of an entry it does not own is
+// neither summed nor stored.
+template <class T, int VEC, int CH>
+__device__ __forceinline__ void store_row(void *p, int64_t at, const Columns<VEC, CH> &k,
+                                          const float (&v)[CH * VEC]) {
+    T *row = static_cast<T *>(p) + at;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        float x[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[e] = v[j * VEC + e];
+        if (k.skip[j] == 0) {
+            Pack<T, VEC>::store(row + k.col[j], x);
+        } else {
+#pragma unroll
+            for (int e = 1; e < VEC; ++e)
+                if (k.counts(j, e)) {
+                    const float y[1] = {x[e]};
+                    Pack<T, 1>::store(row + k.col[j] + e, y);
+                }
+        }
+    }
+}
+
+template <int VEC, int CH>
+__device__ __forceinline__ void load_param(const float *p, float otherwise, const Columns<VEC, CH> &k,
+                                           float (&v)[CH * VEC]) {
+    if (p) {
+        load_row<float, VEC, CH>(p, 0, k, v);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < CH * VEC; ++i) v[i] = otherwise;
+}
+
+// mean and reciprocal root of a row (mean 0 for RMS); two passes over the
+// registers for LAYER, so that no digits are lost where the mean is large
+template <int VEC, int CH>
+__device__ __forceinline__ void row_stats(const float (&v)[CH * VEC], const Columns<VEC, CH> &k, int kind, int N,
+                                          float eps, float (*red)[8][4], int &turn, int waves, float &mean,
+                                          float &r) {
+    mean = 0.f;
+    if (kind == COMERA_NORM_LAYER) {
+        float s[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < CH * VEC; ++i) s[0] += k.counts(i / VEC, i % VEC) ? v[i] : 0.f;
+        row_sum<1>(s, red, turn, waves);
+        mean = s[0] / float(N);
+    }
+    float q[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < CH * VEC; ++i) {
+        const float x = v[i] - mean;
+        q[0] += k.counts(i / VEC, i % VEC) ? x * x : 0.f;
+    }
+    row_sum<1>(q, red, turn, waves);
+    r = 1.f / sqrtf(q[0] / float(N) + eps);
+}
+
+template <class TS, class TA, int VEC, int CH>
+__global__ __launch_bounds__(512) void block_norm_fwd_kernel(NormArgs p) {
+    constexpr int NE = VEC * CH;
+    __shared__ float red[2][8][4];
+    int turn = 0;
+    const int waves = p.lpr >> 6, rows = int(blockDim.x) / p.lpr;
+    const int lane = int(threadIdx.x) % p.lpr;
+    const Columns<VEC, CH> k(lane, p.lpr, p.N);
+    float pw[NE], pb[NE], w[NE], wb[NE];
+    load_param<VEC, CH>(p.gate_ch, 1.f, k, pw);
+    load_param<VEC, CH>(p.post_b, 0.f, k, pb);
+#pragma unroll
+    for (int i = 0; i < NE; ++i) pb[i] *= pw[i];
+    {
+        float x[NE];
+        load_param<VEC, CH>(p.post_w, 1.f, k, x);
+#pragma unroll
+        for (int i = 0; i < NE; ++i) pw[i] *= x[i];
+    }
+    load_param<VEC, CH>(p.pre_w, 1.f, k, w);
+    load_param<VEC, CH>(p.pre_b, 0.f, k, wb);
+    for (int64_t row = int64_t(blockIdx.x) * rows + int(threadIdx.x) / p.lpr; row < p.b;
+         row += int64_t(gridDim.x) * rows) {
+        const int64_t at = row * p.N;
+        float x[NE];
+        load_row<TS, VEC, CH>(p.X, at, k, x);
+        if (p.F) {
+            float f[NE];
+            load_row<TA, VEC, CH>(p.F, at, k, f);
+            float mean = 0.f, r = 1.f;
+            if (p.post != COMERA_NORM_NONE)
+                row_stats<VEC, CH>(f, k, p.post, p.N, p.eps, red, turn, waves, mean, r);
+            float z[NE];
+#pragma unroll
+            for (int i = 0; i < NE; ++i) z[i] = (f[i] - mean) * r * pw[i] + pb[i];
+            if (p.gate) {
+                float g[NE];
+                load_row<TA, VEC, CH>(p.gate, at, k, g);
+#pragma unroll
+                for (int i = 0; i < NE; ++i) z[i] *= g[i];
+            }
+#pragma unroll
+            for (int i = 0; i < NE; ++i) x[i] = p.a * x[i] + p.beta * z[i];
+        }
+        // the pre-norm takes Xn before its rounding to the stream's type
+        float mean = 0.f, r = 1.f;
+        if (p.pre != COMERA_NORM_NONE) row_stats<VEC, CH>(x, k, p.pre, p.N, p.eps, red, turn, waves, mean, r);
+        if (p.Xn) store_row<TS, VEC, CH>(p.Xn, at, k, x);
+        if (p.H) {
+#pragma unroll
+            for (int i = 0; i < NE; ++i) x[i] = (x[i] - mean) * r * w[i] + wb[i];
+            store_row<TA, VEC, CH>(p.H, at, k, x);
+        }
+    }
+}
+
+// Sums over the tokens that the parameters' gradients need, kept in
+// registers over the rows of a workgroup: of y_F times T (times the token's
+// gate), of T alike, of dH times y_X and of dH; the second and the fourth
+// only with BIAS.  finish_kernel adds the workgroups' sums in order.
+template <class TS, class TA, int VEC, int CH, bool BIAS>
+__global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
+    constexpr int NE = VEC * CH, NS = BIAS ? 4 : 2;
+    __shared__ float red[2][8][4];
+    extern __shared__ float share[];       // [rows][N] when rows > 1
+    int turn = 0;
+    const int waves = p.lpr >> 6, rows = int(blockDim.x) / p.lpr;
+    const int lane = int(threadIdx.x) % p.lpr;
+    const Columns<VEC, CH> k(lane, p.lpr, p.N);
+    const float inv_n = 1.f / float(p.N);
+    float pw[NE], w[NE], acc[NS][NE];
+    load_param<VEC, CH>(p.gate_ch, 1.f, k, pw);
+    {
+        float x[NE];
+        load_param<VEC, CH>(p.post_w, 1.f, k, x);
+#pragma unroll
+        for (int i = 0; i < NE; ++i) pw[i] *= p.beta * x[i];
+    }
+    load_param<VEC, CH>(p.pre_w, 1.f, k, w);
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int i = 0; i < NE; ++i) acc[s][i] = 0.f;
+    for (int64_t row = int64_t(blockIdx.x) * rows + int(threadIdx.x) / p.lpr; row < p.b;
+         row += int64_t(gridDim.x) * rows) {
+        const int64_t at = row * p.N;
+        float t[NE];
+        if (p.dXn) {
+            load_row<TS, VEC, CH>(p.dXn, at, k, t);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NE; ++i) t[i] = 0.f;
+        }
+        if (p.dH) {
+            float x[NE], h[NE], mean, r;
+            load_row<TS, VEC, CH>(p.X, at, k, x);
+            load_row<TA, VEC, CH>(p.dH, at, k, h);
+            row_stats<VEC, CH>(x, k, p.pre, p.N, p.eps, red, turn, waves, mean, r);
+            float s[2] = {0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < NE; ++i) {
+                x[i] = (x[i] - mean) * r;
+                acc[0 + NS / 2][i] += h[i] * x[i];
+                if constexpr (BIAS) acc[3][i] += h[i];
+                h[i] *= w[i];
+                s[0] += k.counts(i / VEC, i % VEC) ? h[i] * x[i] : 0.f;
+                s[1] += k.counts(i / VEC, i % VEC) ? h[i] : 0.f;
+            }
+            row_sum<2>(s, red, turn, waves);
+            const float sy = s[0] * inv_n, su = p.pre == COMERA_NORM_LAYER ? s[1] * inv_n : 0.f;
+#pragma unroll
+            for (int i = 0; i < NE; ++i) t[i] += r * (h[i] - su - x[i] * sy);
+        }
+        if (p.dX) {
+            float x[NE];
+#pragma unroll
+            for (int i = 0; i < NE; ++i) x[i] = p.F ? p.a * t[i] : t[i];
+            store_row<TS, VEC, CH>(p.dX, at, k, x);
+        }
+        if (!p.F) continue;
+        float f[NE], mean = 0.f, r = 1.f;
+        load_row<TA, VEC, CH>(p.F, at, k, f);
+        if (p.post != COMERA_NORM_NONE) {
+            row_stats<VEC, CH>(f, k, p.post, p.N, p.eps, red, turn, waves, mean, r);
+#pragma unroll
+            for (int i = 0; i < NE; ++i) f[i] = (f[i] - mean) * r;
+        }
+        if (p.gate) {
+            float g[NE], z[NE], x[NE];
+            load_row<TA, VEC, CH>(p.gate, at, k, g);
+            load_param<VEC, CH>(p.post_w, 1.f, k, z);
+            load_param<VEC, CH>(p.post_b, 0.f, k, x);
+#pragma unroll
+            for (int i = 0; i < NE; ++i) {
+                z[i] = p.beta * t[i] * (f[i] * z[i] + x[i]);
+                t[i] *= g[i];
+            }
+            if (p.dgate) store_row<TA, VEC, CH>(p.dgate, at, k, z);
+        }
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NE; ++i) {
+            acc[0][i] += t[i] * f[i];
+            if constexpr (BIAS) acc[1][i] += t[i];
+            t[i] *= pw[i];
+            s[0] += k.counts(i / VEC, i % VEC) ? t[i] * f[i] : 0.f;
+            s[1] += k.counts(i / VEC, i % VEC) ? t[i] : 0.f;
+        }
+        if (p.post != COMERA_NORM_NONE) {
+            row_sum<2>(s, red, turn, waves);
+            const float sy = s[0] * inv_n, su = p.post == COMERA_NORM_LAYER ? s[1] * inv_n : 0.f;
+#pragma unroll
+            for (int i = 0; i < NE; ++i) t[i] = r * (t[i] - su - f[i] * sy);
+        }
+        if (p.dF) store_row<TA, VEC, CH>(p.dF, at, k, t);
+    }
+    if (!p.part) return;
+    // the workgroup's sums: its rows added in order through LDS
+    float *out = p.part + int64_t(blockIdx.x) * NS * p.N;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        if (rows == 1) {
+            store_row<float, VEC, CH>(out, int64_t(s) * p.N, k, acc[s]);
+            continue;
+        }
+        store_row<float, VEC, CH>(share, int64_t(threadIdx.x / p.lpr) * p.N, k, acc[s]);
+        __syncthreads();
+        for (int c = threadIdx.x; c < p.N; c += int(blockDim.x)) {
+            float v = share[c];
+            for (int x = 1; x < rows; ++x) v += share[x * p.N + c];
+            out[s * p.N + c] = v;
+        }
+        __syncthreads();
+    }
+}
+
+struct FinishArgs {
+    const float *part;
+    int parts, sums, N, post, token_gate;
+    const float *gate_ch, *post_w, *post_b;
+    float beta;
+    float *dgate, *dpost_w, *dpost_b, *dpre_w, *dpre_b;
+};
+
+constexpr int kFinCols = 16, kFinGroups = 16;
+
+// Sums of the workgroups' partials and the parameters' gradients from them.
+// 16 columns x 16 groups of partials per workgroup, the groups added in order.
+__global__ __launch_bounds__(kFinCols *kFinGroups) void block_norm_finish_kernel(FinishArgs a) {
+    __shared__ float red[4][kFinGroups][kFinCols];
+    const int l = threadIdx.x % kFinCols, g = threadIdx.x / kFinCols;
+    const int c = blockIdx.x * kFinCols + l;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c < a.N)
+        for (int p = g; p < a.parts; p += kFinGroups)
+            for (int s = 0; s < a.sums; ++s) v[s] += a.part[(int64_t(p) * a.sums + s) * a.N + c];
+    for (int s = 0; s < 4; ++s) red[s][g][l] = v[s];
+    __syncthreads();
+    if (g != 0 || c >= a.N) return;
+    for (int s = 0; s < 4; ++s)
+        for (int x = 1; x < kFinGroups; ++x) v[s] += red[s][x][l];
+    const float yT = v[0], T = a.sums == 4 ? v[1] : 0.f, yH = v[a.sums / 2], H = v[3];
+    const float gate = a.gate_ch ? a.gate_ch[c] : 1.f;
+    if (a.dpost_w) a.dpost_w[c] = a.beta * gate * yT;
+    if (a.dpost_b) a.dpost_b[c] = a.beta * gate * T;
+    if (a.dgate)
+        a.dgate[c] = a.beta * (yT * (a.post_w ? a.post_w[c] : 1.f) + (a.post_b ? a.post_b[c] * T : 0.f));
+    if (a.dpre_w) a.dpre_w[c] = yH;
+    if (a.dpre_b) a.dpre_b[c] = H;
+}
+
+// ---------------------------------------------------------------- host side
+bool norm_kind(int k) { return k == COMERA_NORM_NONE || k == COMERA_NORM_RMS || k == COMERA_NORM_LAYER; }
+
+bool norm_shape_ok(const comera_block_norm_shape *s) {
+    return s && s->width >= 1 && (s->stream == COMERA_F32 || s->stream == COMERA_BF16) &&
+           (s->act == COMERA_F32 || s->act == COMERA_BF16) && norm_kind(s->post) && norm_kind(s->pre) &&
+           (s->gate == COMERA_GATE_NONE || s->gate == COMERA_GATE_CHANNEL || s->gate == COMERA_GATE_TOKEN) &&
+           std::isfinite(s->eps) && s->eps > 0.f && std::isfinite(s->res_scale) && std::isfinite(s->branch_scale);
+}
+
+// a bf16 stream between fp32 blocks has no kernels
+bool norm_supported(const comera_block_norm_shape *s) {
+    return s->width <= kMaxWidth && !(s->stream == COMERA_BF16 && s->act == COMERA_F32);
+}
+
+// How a row is spread: lanes per row and entries per lane.
+struct Spread {
+    int vec, ch, lpr;
+    int rows() const { return lpr == 64 ? kWaveRows : 1; }
+    int threads() const { return lpr == 64 ? 64 * kWaveRows : lpr; }
+};
+
+// 8 entries a lane up to 512 columns; above, 12 or 16, whichever leaves fewer
+// idle lanes (768 columns: 64 lanes x 12); single entries below 8 columns
+Spread spread_of(int N) {
+    if (N < 8) return {1, 1, 64};
+    if (N <= 512) return {8, 1, 64};
+    const int l12 = (N + 767) / 768 * 64, l16 = (N + 1023) / 1024 * 64;
+    if (l12 * 12 < l16 * 16 && l12 <= 512) return {4, 3, l12};
+    return {8, 2, l16};
+}
+
+int64_t bwd_parts(const Spread &sp, int64_t b) {
+    return std::min<int64_t>((b + sp.rows() - 1) / sp.rows(), kMaxParts);
+}
+
+template <class TS, class TA>
+void launch_fwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
+    const unsigned grid = unsigned(std::min<int64_t>((p.b + sp.rows() - 1) / sp.rows(), 4096));
+    const dim3 block(sp.threads());
+    if (sp.vec == 1)
+        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 1, 1>), dim3(grid), block, 0, st, p);
+    else if (sp.vec == 4)
+        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 4, 3>), dim3(grid), block, 0, st, p);
+    else if (sp.ch == 1)
+        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 8, 1>), dim3(grid), block, 0, st, p);
+    else
+        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 8, 2>), dim3(grid), block, 0, st, p);
+}
+
+template <class TS, class TA, bool BIAS>
+void launch_bwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
+    const unsigned grid = unsigned(bwd_parts(sp, p.b));
+    const dim3 block(sp.threads());
+    const size_t lds = sp.rows() > 1 ? sizeof(float) * sp.rows() * p.N : 0;
+    if (sp.vec == 1)
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 1, 1, BIAS>), dim3(grid), block, lds, st, p);
+    else if (sp.vec == 4)
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 4, 3, BIAS>), dim3(grid), block, lds, st, p);
+    else if (sp.ch == 1)
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 1, BIAS>), dim3(grid), block, lds, st, p);
+    else
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 2, BIAS>), dim3(grid), block, lds, st, p);
+}
+
+}  // namespace
+}  // namespace comera
+
+using namespace comera;
+
+extern "C" {
+
+size_t comera_block_norm_workspace_bytes(const comera_block_norm_shape *s, int64_t b) {
+    if (!norm_shape_ok(s) || !norm_supported(s) || b < 0) return 0;
+    return sizeof(float) * 4 * size_t(s->width) * size_t(std::max<int64_t>(1, bwd_parts(spread_of(int(s->width)), b)));
+}
+
+comera_status comera_block_norm_forward(const comera_block_norm_shape *s, int64_t b, const void *X, const void *F,
+                                        const float *post_w, const float *post_b, const void *gate, const float *pre_w,
+                                        const float *pre_b, void *Xn, void *H, void *stream) {
+    if (!norm_shape_ok(s) || b < 0) return COMERA_ERR_INVALID_ARG;
+    if (!norm_supported(s)) return COMERA_ERR_UNSUPPORTED;
+    const bool gated = s->gate != COMERA_GATE_NONE;
+    // what the shape leaves out is not passed, what it names is
+    if ((!F && b > 0 && (Xn || post_w || post_b || gate)) || (F && gated != (gate != nullptr)) ||
+        (s->post == COMERA_NORM_NONE && (post_w || post_b)) || (s->pre == COMERA_NORM_NONE && (pre_w || pre_b || H)) ||
+        (s->pre != COMERA_NORM_NONE && !H && b > 0))
+        return COMERA_ERR_INVALID_ARG;
+    if (b == 0) return COMERA_OK;
+    if (!X || (!Xn && !H)) return COMERA_ERR_INVALID_ARG;
+    NormArgs p{};
+    p.X = X;
+    p.F = F;
+    if (gated && s->gate == COMERA_GATE_CHANNEL) p.gate_ch = static_cast<const float *>(gate);
+    if (gated && s->gate == COMERA_GATE_TOKEN) p.gate = gate;
+    p.post_w = post_w;
+    p.post_b = post_b;
+    p.pre_w = pre_w;
+    p.pre_b = pre_b;
+    p.Xn = Xn;
+    p.H = H;
+    p.b = b;
+    p.N = int(s->width);
+    p.post = s->post;
+    p.pre = s->pre;
+    p.eps = s->eps;
+    p.a = s->res_scale;
+    p.beta = s->branch_scale;
+    const Spread sp = spread_of(p.N);
+    p.lpr = sp.lpr;
+    hipStream_t st = hipStream_t(stream);
+    if (s->stream == COMERA_F32 && s->act == COMERA_F32)
+        launch_fwd<float, float>(p, sp, st);
+    else if (s->stream == COMERA_F32)
+        launch_fwd<float, bf16>(p, sp, st);
+    else
+        launch_fwd<bf16, bf16>(p, sp, st);
+    return note_hip(launch_status(), "block norm") ? COMERA_ERR_HIP : COMERA_OK;
+}
+
+comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64_t b, const void *Xn, const void *F,
+                                         const float *post_w, const float *post_b, const void *gate,
+                                         const float *pre_w, const void *dXn, const void *dH, void *dX, void *dF,
+                                         void *dgate, float *dpost_w, float *dpost_b, float *dpre_w, float *dpre_b,
+                                         void *ws, size_t ws_bytes, void *stream) {
+    if (!norm_shape_ok(s) || b < 0) return COMERA_ERR_INVALID_ARG;
+    if (!norm_supported(s)) return COMERA_ERR_UNSUPPORTED;
+    const bool gated = s->gate != COMERA_GATE_NONE, channel = s->gate == COMERA_GATE_CHANNEL;
+    const bool pre = s->pre != COMERA_NORM_NONE, post = s->post != COMERA_NORM_NONE;
+    if ((!F && b > 0 && (dF || dgate || dpost_w || dpost_b || post_w || post_b || gate)) ||
+        (F && gated != (gate != nullptr)) || (!gated && dgate) ||
+        (!post && (post_w || post_b || dpost_w || dpost_b)) || (!pre && (pre_w || dpre_w || dpre_b || dH)))
+        return COMERA_ERR_INVALID_ARG;
+    const bool params = dpost_w || dpost_b || dpre_w || dpre_b || (channel && dgate);
+    const Spread sp = spread_of(int(s->width));
+    const int64_t parts = bwd_parts(sp, b);
+    if (b > 0 && ((!dXn && !dH) || (dH && !Xn))) return COMERA_ERR_INVALID_ARG;
+    if (params && b > 0 &&
+        (!ws || ws_bytes < comera_block_norm_workspace_bytes(s, b) || reinterpret_cast<uintptr_t>(ws) % 8))
+        return COMERA_ERR_WORKSPACE;
+    hipStream_t st = hipStream_t(stream);
+    // the sums of T and of dH are formed only where a bias needs them
+    const bool bias = dpost_b || dpre_b || (channel && dgate && post_b);
+    NormArgs p{};
+    p.X = Xn;
+    p.F = F;
+    if (channel) p.gate_ch = static_cast<const float *>(gate);
+    if (s->gate == COMERA_GATE_TOKEN) p.gate = gate;
+    p.post_w = post_w;
+    p.post_b = post_b;
+    p.pre_w = pre_w;
+    p.dXn = dXn;
+    p.dH = dH;
+    p.dX = dX;
+    p.dF = dF;
+    if (!channel) p.dgate = dgate;
+    p.part = params ? static_cast<float *>(ws) : nullptr;
+    p.b = b;
+    p.N = int(s->width);
+    p.post = s->post;
+    p.pre = s->pre;
+    p.eps = s->eps;
+    p.a = s->res_scale;
+    p.beta = s->branch_scale;
+    p.lpr = sp.lpr;
+    if (b > 0 && (params || dX || dF || p.dgate)) {
+        if (s->stream == COMERA_F32 && s->act == COMERA_F32)
+            bias ? launch_bwd<float, float, true>(p, sp, st) : launch_bwd<float, float, false>(p, sp, st);
+        else if (s->stream == COMERA_F32)
+            bias ? launch_bwd<float, bf16, true>(p, sp, st) : launch_bwd<float, bf16, false>(p, sp, st);
+        else
+            bias ? launch_bwd<bf16, bf16, true>(p, sp, st) : launch_bwd<bf16, bf16, false>(p, sp, st);
+    }
+    if (params) {
+        FinishArgs f{};
+        f.part = p.part;
+        f.parts = int(parts);
+        f.sums = bias ? 4 : 2;
+        f.N = p.N;
+        f.gate_ch = p.gate_ch;
+        f.post_w = post_w;
+        f.post_b = post_b;
+        f.beta = p.beta;
+        f.dgate = channel ? static_cast<float *>(dgate) : nullptr;
+        f.dpost_w = dpost_w;
+        f.dpost_b = dpost_b;
+        f.dpre_w = dpre_w;
+        f.dpre_b = dpre_b;
+        COMERA_LAUNCH(block_norm_finish_kernel, dim3(unsigned((p.N + kFinCols - 1) / kFinCols)),
+                      dim3(kFinCols * kFinGroups), 0, st, f);
+    }
+    return note_hip(launch_status(), "block norm") ? COMERA_ERR_HIP : COMERA_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,329 @@
+"""Norms around a block on the GPU against the fp64 oracle.
+
+Tolerances, in half steps u = 2^-24 of fp32: a sum over a row is at most 16
+products in a lane, 6 exchanges and 8 waves (32 roundings), so a normalised
+entry y is off by less than 64 u of My, a bound of the magnitudes that form
+it (My is larger than |y| where the mean is large against the spread); the
+operations behind it (weights, gate, scales, residual) add less than 16 u of
+the magnitudes that they join.  The backward does this twice, one norm's
+result entering the other.  Sums over the rows of a batch add at most
+(rows of one workgroup) + 64 roundings.  Outputs in bf16 add half a step.
+"""
+import numpy as np
+import pytest
+
+from oracle import block_norm as ON
+from paper_2405_14377_amd import comera as C
+from tests.step_util import HALF, U, Guarded, dev, values, within
+
+pytestmark = pytest.mark.gpu
+
+CODE = {"f32": C.F32, "bf16": C.BF16}
+KIND = {"none": C.NORM_NONE, "rms": C.NORM_RMS, "layer": C.NORM_LAYER}
+GATE = {"none": C.GATE_NONE, "channel": C.GATE_CHANNEL, "token": C.GATE_TOKEN}
+TYPES = [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")]
+EPS = 1e-5
+NAMES = ("dX", "dF", "dgate", "dpost_w", "dpost_b", "dpre_w", "dpre_b")
+
+
+def f32(x):
+    return float(np.float32(x))
+
+
+class Case:
+    def __init__(self, b, n, types, post, pre, gate, seed=0, mean=0.0, bias=True, res=0.9, branch=0.7, block=True):
+        rng = np.random.default_rng(seed + 7 * b + n)
+        self.b, self.n, (self.st, self.act) = b, n, types
+        self.post, self.pre, self.gate_kind, self.block = post, pre, gate, block
+        self.a, self.beta, self.eps = f32(res), f32(branch), f32(EPS)
+
+        def rows(dtype, scale=1.0, m=0.0):
+            return values(m + scale * rng.standard_normal((b, n)), dtype)
+
+        def par(m):
+            return values(m + 0.3 * rng.standard_normal(n), "f32")
+
+        self.X = rows(self.st, 1.0, mean)
+        self.F = rows(self.act, 2.0, mean) if block else None
+        self.post_w = par(1) if block and post != "none" else None
+        self.post_b = par(0) if block and post != "none" and bias else None
+        self.pre_w = par(1) if pre != "none" else None
+        self.pre_b = par(0) if pre != "none" and bias else None
+        self.gate = None if gate == "none" or not block else par(1) if gate == "channel" else rows(self.act)
+        self.dXn = rows(self.st)
+        self.dH = rows(self.act) if pre != "none" else None
+        self.shape = C.block_norm_shape(n, CODE[self.st], CODE[self.act], KIND[post], KIND[pre], GATE[gate], EPS, res,
+                                        branch)
+
+    def gate_type(self):
+        return self.act if self.gate_kind == "token" else "f32"
+
+    def dev_in(self, offset=0):
+        d = {k: None if v is None else dev(v) for k, v in (("post_w", self.post_w), ("post_b", self.post_b),
+                                                           ("pre_w", self.pre_w), ("pre_b", self.pre_b))}
+        d["X"], d["F"] = dev(self.X, self.st, offset), None if self.F is None else dev(self.F, self.act, offset)
+        d["gate"] = None if self.gate is None else dev(self.gate, self.gate_type(), offset)
+        d["dXn"] = None if self.dXn is None else dev(self.dXn, self.st, offset)
+        d["dH"] = None if self.dH is None else dev(self.dH, self.act, offset)
+        return d
+
+    def oracle_forward(self):
+        return ON.forward(self.X, self.F, self.post, self.post_w, self.post_b, self.gate, self.pre, self.pre_w,
+                          self.pre_b, self.eps, self.a, self.beta)
+
+    def oracle_backward(self):
+        return ON.backward(self.X, self.F, self.post, self.post_w, self.post_b, self.gate, self.pre, self.pre_w,
+                           self.dXn, self.dH, self.eps, self.a, self.beta)
+
+    # -------- bounds of the errors
+    def _my(self, v, kind):
+        """(bound of the magnitudes behind the normalised entries, reciprocal roots)."""
+        y, r = ON.normalise(v, kind, self.eps)
+        if kind == "none":
+            return np.abs(y), r
+        m = r * (np.abs(v) + (np.mean(np.abs(v), axis=1, keepdims=True) if kind == "layer" else 0))
+        return m + np.abs(y) * np.sqrt(np.mean(m * m, axis=1, keepdims=True)), r
+
+    @staticmethod
+    def _abs(x, otherwise):
+        return otherwise if x is None else np.abs(x)
+
+    def bound_forward(self, Xn, H):
+        mz = 0.0
+        if self.F is not None:
+            my, _ = self._my(self.F, self.post)
+            mz = (my * self._abs(self.post_w, 1.0) + self._abs(self.post_b, 0.0)) * self._abs(self.gate, 1.0)
+        mx = self.a * np.abs(self.X) + self.beta * mz if self.F is not None else np.abs(self.X)
+        ex = (80 * U if self.F is not None else 0.0) * mx
+        bx = ex + HALF[self.st] * np.abs(Xn) * 1.001
+        if H is None:
+            return bx, None
+        my, r = self._my(Xn, self.pre)
+        spread = np.sqrt(np.mean(ex * ex, axis=1, keepdims=True))
+        ey = 80 * U * my + r * (ex + spread) + np.abs(my) * r * spread
+        return bx, ey * self._abs(self.pre_w, 1.0) + 2 * U * self._abs(self.pre_b, 0.0) + \
+            HALF[self.act] * np.abs(H) * 1.001
+
+    def bound_backward(self, ref):
+        def vjp(r, u, my, kind):      # magnitudes of a norm's gradient
+            if kind == "none":
+                return u
+            return r * (u + my * np.mean(u * my, axis=1, keepdims=True) + np.mean(u, axis=1, keepdims=True))
+
+        K = 160 * U
+        rows = self.b / 256 + 4 + 64
+        out = {}
+        mt = self._abs(self.dXn, 0.0) * np.ones(self.X.shape)
+        if self.pre != "none":
+            my, r = self._my(self.X, self.pre)
+            dh = self._abs(self.dH, 0.0) * np.ones(self.X.shape)
+            mt = mt + vjp(r, dh * self._abs(self.pre_w, 1.0), my, self.pre)
+            out["dpre_w"] = (K + rows * U) * np.sum(dh * my, axis=0)
+            out["dpre_b"] = rows * U * np.sum(dh, axis=0)
+        out["dX"] = K * mt * (self.a if self.block else 1.0) + HALF[self.st] * np.abs(ref["dX"]) * 1.001
+        if self.block:
+            my, r = self._my(self.F, self.post)
+            mz = my * self._abs(self.post_w, 1.0) + self._abs(self.post_b, 0.0)
+            dz = self.beta * mt * self._abs(self.gate, 1.0)
+            if self.gate is not None:
+                dg = self.beta * mt * mz
+                if self.gate.ndim == 1:
+                    out["dgate"] = (2 * K + rows * U) * dg.sum(axis=0)
+                else:
+                    out["dgate"] = 2 * K * dg + HALF[self.act] * np.abs(ref["dgate"]) * 1.001
+            out["dF"] = 2 * K * vjp(r, dz * self._abs(self.post_w, 1.0), my, self.post) + \
+                HALF[self.act] * np.abs(ref["dF"]) * 1.001
+            if self.post != "none":
+                out["dpost_w"] = (2 * K + rows * U) * np.sum(dz * my, axis=0)
+                out["dpost_b"] = (K + rows * U) * np.sum(dz, axis=0)
+        return out
+
+    # -------- runs
+    def forward(self, offset=0):
+        d = self.dev_in(offset)
+        Xn = Guarded((self.b, self.n), self.st, offset) if self.block else None
+        H = Guarded((self.b, self.n), self.act, offset) if self.pre != "none" else None
+        C.comera_block_norm_forward(self.shape, self.b, d["X"], d["F"], d["post_w"], d["post_b"], d["gate"],
+                                    d["pre_w"], d["pre_b"], Xn and Xn.t, H and H.t)
+        return Xn, H
+
+    def backward(self, offset=0, leave_out=(), d=None, ws=None):
+        import torch
+        d = d or self.dev_in(offset)
+        ref = self.oracle_backward()
+        out = {}
+        for k in ref:
+            if k in leave_out or (k == "dpost_b" and self.post_b is None) or (k == "dpre_b" and self.pre_b is None):
+                continue
+            kind = self.st if k == "dX" else self.act if k == "dF" else self.gate_type() if k == "dgate" else "f32"
+            out[k] = Guarded(ref[k].shape, kind, offset if k in ("dX", "dF") else 0)
+        if ws is None:
+            ws = torch.full((C.comera_block_norm_workspace_bytes(self.shape, self.b),), 0xA5, dtype=torch.uint8,
+                            device="cuda")
+        o = [out[k].t if k in out else None for k in NAMES]
+        C.comera_block_norm_backward(self.shape, self.b, d["X"], d["F"], d["post_w"], d["post_b"], d["gate"],
+                                     d["pre_w"], d["dXn"], d["dH"], *o, ws)
+        return out, ref
+
+    def check_forward(self, offset=0):
+        Xn, H = self.forward(offset)
+        rx, rh = self.oracle_forward()
+        bx, bh = self.bound_forward(rx, rh)
+        if Xn:
+            within(Xn.np(), rx, bx)
+        if H:
+            within(H.np(), rh, bh)
+
+    def check_backward(self, offset=0, leave_out=()):
+        out, ref = self.backward(offset, leave_out)
+        bound = self.bound_backward(ref)
+        for k, v in out.items():
+            try:
+                within(v.np(), ref[k], bound[k] + 1e-37)
+            except AssertionError as e:
+                raise AssertionError(f"{k}: {e}") from None
+
+
+WIDTHS = [1, 2, 5, 7, 8, 9, 63, 64, 100, 511, 512, 513, 767, 768, 769, 1001, 1024, 1025, 1536, 1537, 2048, 3000, 4096,
+          5000, 6144, 6145, 8191, 8192]
+
+
+@pytest.mark.parametrize("types", TYPES, ids="-".join)
+@pytest.mark.parametrize("n", WIDTHS)
+def test_widths(n, types):
+    i = WIDTHS.index(n)
+    post, pre, gate = ("rms", "layer", "none")[i % 3], ("layer", "rms")[i % 2], ("channel", "token", "none")[i % 3 - 1]
+    c = Case((1, 3, 9, 34)[i % 4], n, types, post, pre, gate)
+    c.check_forward(offset=i % 3)
+    c.check_backward(offset=i % 3)
+
+
+@pytest.mark.parametrize("post", ["none", "rms", "layer"])
+@pytest.mark.parametrize("pre", ["none", "rms", "layer"])
+@pytest.mark.parametrize("gate", ["none", "channel", "token"])
+@pytest.mark.parametrize("bias", [True, False])
+def test_kinds(post, pre, gate, bias):
+    for n, types in ((96, TYPES[0]), (1100, TYPES[2])):
+        c = Case(11, n, types, post, pre, gate, bias=bias)
+        c.check_forward()
+        c.check_backward()
+
+
+@pytest.mark.parametrize("n", [64, 1001, 4096])
+def test_without_a_block_before(n):
+    for pre in ("rms", "layer"):
+        c = Case(5, n, TYPES[1], "none", pre, "none", block=False)
+        c.check_forward()
+        c.check_backward()
+
+
+@pytest.mark.parametrize("b,n", [(1, 768), (255, 512), (256, 100), (1025, 768), (2100, 256), (700, 1536), (3001, 40)])
+def test_batches(b, n):
+    c = Case(b, n, TYPES[1], "layer", "rms", "channel")
+    c.check_forward()
+    c.check_backward()
+
+
+def test_large_mean():
+    """A mean of 100 spreads: the variance is taken around the mean."""
+    c = Case(6, 768, TYPES[0], "layer", "layer", "token", mean=100.0)
+    c.check_forward()
+    c.check_backward()
+
+
+def test_parts_of_the_backward():
+    base = dict(b=37, n=1001, types=TYPES[2], post="layer", pre="layer", gate="channel")
+    Case(**base).check_backward(leave_out=("dX",))
+    Case(**base).check_backward(leave_out=("dF", "dgate", "dpost_b"))
+    Case(**base).check_backward(leave_out=("dpost_w", "dpost_b", "dpre_w", "dpre_b", "dgate"))
+    c = Case(**base)
+    c.dXn = None
+    c.check_backward()
+    c = Case(**base)
+    c.dH = None
+    c.check_backward()
+
+
+@pytest.mark.parametrize("n", [8, 1001, 1025])
+def test_zero_rows_and_rows_with_infinities(n):
+    """A row of zeros is normalised to zeros (eps), and what one row holds stays in it."""
+    c = Case(7, n, TYPES[0], "rms", "layer", "none", bias=False)
+    c.X[2], c.F[2] = 0.0, 0.0
+    c.X[4, 1] = np.inf
+    c.F[5, n - 1] = np.nan
+    Xn, H = c.forward()
+    xn, h = Xn.t.cpu().numpy(), H.t.cpu().numpy()
+    assert not xn[2].any() and not h[2].any()
+    assert np.isnan(h[4]).any() and np.isnan(xn[5, n - 1]) and np.isnan(h[5]).all()
+    rest = [0, 1, 3, 6]
+    assert np.isfinite(xn[rest]).all() and np.isfinite(h[rest]).all()
+
+
+@pytest.mark.parametrize("n", [96, 1001, 1030, 5001])
+def test_outputs_over_inputs(n):
+    import torch
+    c = Case(50, n, TYPES[2], "rms", "rms", "token", bias=False)
+    Xn, H = c.forward()
+    d = c.dev_in(1)
+    C.comera_block_norm_forward(c.shape, c.b, d["X"], d["F"], d["post_w"], None, d["gate"], d["pre_w"], None, d["X"],
+                                d["F"])
+    assert torch.equal(d["X"], Xn.t) and torch.equal(d["F"], H.t)
+    want, _ = c.backward()
+    d = c.dev_in(1)
+    ws = torch.empty(C.comera_block_norm_workspace_bytes(c.shape, c.b), dtype=torch.uint8, device="cuda")
+    dw = [torch.empty(n, device="cuda") for _ in range(2)]
+    C.comera_block_norm_backward(c.shape, c.b, d["X"], d["F"], d["post_w"], None, d["gate"], d["pre_w"], d["dXn"],
+                                 d["dH"], d["dXn"], d["F"], d["gate"], dw[0], None, dw[1], None, ws)
+    for k, t in (("dX", d["dXn"]), ("dF", d["F"]), ("dgate", d["gate"]), ("dpost_w", dw[0]), ("dpre_w", dw[1])):
+        assert torch.equal(t, want[k].t), k
+    # neither norm: nothing of a row is waited for
+    c = Case(50, n, TYPES[2], "none", "none", "none")
+    Xn, _ = c.forward()
+    d = c.dev_in(1)
+    C.comera_block_norm_forward(c.shape, c.b, d["X"], d["F"], None, None, None, None, None, d["X"], None)
+    assert torch.equal(d["X"], Xn.t)
+    want, _ = c.backward()
+    d = c.dev_in(1)
+    C.comera_block_norm_backward(c.shape, c.b, None, d["F"], None, None, None, None, d["dXn"], None, d["dXn"], d["F"],
+                                 None, None, None, None, None, None)
+    assert torch.equal(d["dXn"], want["dX"].t) and torch.equal(d["F"], want["dF"].t)
+
+
+def test_repeatable_and_empty_batch():
+    import torch
+    c = Case(2000, 264, TYPES[1], "layer", "layer", "channel")
+    a, _ = c.backward()
+    for _ in range(2):
+        b, _ = c.backward()
+        assert all(torch.equal(a[k].t, b[k].t) for k in a)
+    out = [Guarded((264,), "f32") for _ in range(5)]
+    C.comera_block_norm_backward(c.shape, 0, None, None, None, None, None, None, None, None, None, None, out[0].t,
+                                 out[1].t, out[2].t, out[3].t, out[4].t, None)
+    assert all(not o.np().any() for o in out)
+
+
+def test_gradients_by_differences():
+    """<forward, cotangents> in fp32 along random directions against the backward."""
+    c = Case(4, 40, TYPES[0], "layer", "rms", "channel", seed=3)
+    Xn0, _ = c.oracle_forward()
+    g = Case(4, 40, TYPES[0], "layer", "rms", "channel", seed=3)
+    g.X = values(Xn0, "f32")
+    out, _ = g.backward()
+    rng = np.random.default_rng(4)
+
+    def loss():
+        Xn, H = c.forward()
+        return float(np.sum(Xn.np() * g.dXn) + np.sum(H.np() * g.dH))
+
+    for name in ("X", "F", "gate", "post_w", "post_b", "pre_w", "pre_b"):
+        x0 = getattr(c, name)
+        step = rng.standard_normal(x0.shape)
+        v = []
+        for h in (1e-2, -1e-2):
+            setattr(c, name, values(x0 + h * step, "f32"))
+            v.append(loss())
+        setattr(c, name, x0)
+        want = float(np.sum(out["d" + name].np() * step))
+        # differences: third-order terms (1e-4 relative to the curvature of
+        # these smooth functions) and fp32 noise of the 320 outputs over 2e-2
+        assert (v[0] - v[1]) / 2e-2 == pytest.approx(want, rel=2e-2, abs=2e-2), name

@@ -1,0 +1,128 @@
+"""Global gradient norm and clipping on the GPU against the fp64 oracle.
+
+Tolerances: the norm is formed in 64 bits and rounded once (half a step of
+fp32, twice that for a subnormal-free bound); a clipped entry is one fp32
+product with a factor that is itself rounded once, then its type's rounding.
+"""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import grad_clip as OG
+from paper_2405_14377_amd import comera as C
+from tests.step_util import HALF, U, Guarded, dev, values, within
+
+pytestmark = pytest.mark.gpu
+
+
+def _tensors(rng, sizes, dtypes):
+    return [values(rng.standard_normal(n) * 10.0 ** rng.integers(-3, 2), dt) for n, dt in zip(sizes, dtypes)]
+
+
+def _run(grads, dtypes, scale, max_norm, in_place=False, offset=0):
+    import torch
+    g = [dev(x, dt, (offset + i) % 4) for i, (x, dt) in enumerate(zip(grads, dtypes))]
+    outs = None if in_place else [Guarded(x.shape, dt, i % 3) for i, (x, dt) in enumerate(zip(grads, dtypes))]
+    plan = C.GradPlan(g, None if in_place else [o.t for o in outs])
+    ws = torch.full((plan.workspace_bytes,), 0xFF, dtype=torch.uint8, device="cuda")
+    norm, flag = torch.zeros(1, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    C.comera_grad_clip(plan.handle, scale, max_norm, norm, flag, ws)
+    got = [x.double().cpu().numpy() for x in g] if in_place else [o.np() for o in outs]
+    alone = torch.zeros(1, device="cuda")
+    if not in_place:
+        C.comera_grad_norm(plan.handle, scale, alone, None, ws)
+        assert torch.equal(alone, norm) or (torch.isnan(alone) and torch.isnan(norm))
+    return norm.item(), flag.item(), got
+
+
+SIZES = {"one": [1], "odd": [3, 1, 0, 17, 8193, 30], "tiles": [8192, 8191, 16385, 5], "many": [1 + 37 * i % 501 for i in range(300)],
+         "exactly a launch": [7] * 128, "one more": [7] * 129, "large": [3_000_017, 11, 700_001]}
+
+
+@pytest.mark.parametrize("sizes", list(SIZES))
+@pytest.mark.parametrize("mix", ["f32", "bf16", "both"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_clip(sizes, mix, in_place):
+    rng = np.random.default_rng(1)
+    n = SIZES[sizes]
+    dtypes = [mix if mix != "both" else ("f32", "bf16")[i % 2] for i in range(len(n))]
+    grads = _tensors(rng, n, dtypes)
+    for scale, max_norm in ((1.0, 0.25), (0.125, 1e9), (1.0, 1e9), (2.0, 0.0)):
+        ref_norm, ref = OG.clip(grads, scale, max_norm)
+        norm, flag, got = _run(grads, dtypes, scale, max_norm, in_place)
+        assert norm == pytest.approx(ref_norm, rel=2 * U) and flag == 0
+        for g, r, dt in zip(got, ref, dtypes):
+            within(g, r, (3 * U + (HALF[dt] if dt == "bf16" else 0)) * np.abs(r) * 1.001 + 1e-45)
+
+
+def test_untouched_in_place_below_the_bound():
+    rng = np.random.default_rng(2)
+    grads, dtypes = _tensors(rng, [1000, 77], ["f32", "bf16"]), ["f32", "bf16"]
+    _, _, got = _run(grads, dtypes, 1.0, math.inf, in_place=True)
+    assert all(np.array_equal(a, b) for a, b in zip(got, grads))
+
+
+def test_squares_outside_fp32():
+    """Entries whose squares overflow or vanish in fp32."""
+    for x in (1e30, 1e-30):
+        grads = [np.full(5000, x), np.full(3, 2 * x)]
+        grads = [values(g, "f32") for g in grads]
+        ref_norm, ref = OG.clip(grads, 1.0, x)
+        norm, flag, got = _run(grads, ["f32"] * 2, 1.0, float(np.float32(x)))
+        assert norm == pytest.approx(ref_norm, rel=2 * U) and flag == 0
+        for g, r in zip(got, ref):
+            assert np.allclose(g, r, rtol=1e-6, atol=0)
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_not_finite(bad):
+    rng = np.random.default_rng(3)
+    grads = _tensors(rng, [5000, 64], ["f32", "f32"])
+    grads[1][7] = bad
+    norm, flag, got = _run(grads, ["f32", "f32"], 0.5, 1.0)
+    assert not math.isfinite(norm) and flag == 1
+    assert np.array_equal(got[0], 0.5 * grads[0])
+    norm, flag, got = _run(grads, ["f32", "f32"], 1.0, 1.0, in_place=True)
+    assert flag == 1 and all(np.array_equal(a, b, equal_nan=True) for a, b in zip(got, grads))
+    # finite entries whose norm does not fit fp32
+    norm, flag, _ = _run([np.full(100, 3e38)], ["f32"], 1.0, 1.0)
+    assert math.isinf(norm) and flag == 1
+
+
+def test_nothing_and_zeros():
+    import torch
+    norm, flag, got = _run([np.zeros(100)], ["bf16"], 1.0, 0.0)
+    assert norm == 0 and flag == 0 and not got[0].any()
+    for plan in (C.GradPlan([]), C.GradPlan([torch.empty(0, device="cuda")])):
+        ws = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+        n = torch.full((1,), 5.0, device="cuda")
+        C.comera_grad_clip(plan.handle, 1.0, 1.0, n, None, ws)
+        assert n.item() == 0
+        C.comera_grad_clip(plan.handle, 1.0, 1.0, None, None, ws)
+        n.fill_(5.0)
+        C.comera_grad_norm(plan.handle, 1.0, n, None, ws)
+        assert n.item() == 0
+
+
+def test_repeatable():
+    rng = np.random.default_rng(4)
+    grads, dtypes = _tensors(rng, [100_003, 555, 70_000], ["f32", "bf16", "f32"]), ["f32", "bf16", "f32"]
+    a = _run(grads, dtypes, 1.0, 0.5)
+    for off in (0, 0):
+        b = _run(grads, dtypes, 1.0, 0.5, offset=off)
+        assert a[0] == b[0] and all(np.array_equal(x, y) for x, y in zip(a[2], b[2]))
+
+
+def test_more_than_2_31_entries():
+    import torch
+    n = (1 << 31) + 12345
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g[-1], g[0], g[1 << 31] = 2.0, 1.0, 2.0
+    plan = C.GradPlan([g])
+    ws = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+    norm = torch.zeros(1, device="cuda")
+    C.comera_grad_clip(plan.handle, 1.0, 1.5, norm, None, ws)
+    assert norm.item() == 3.0
+    assert g[-1].item() == 1.0 and g[0].item() == 0.5 and g[1 << 31].item() == 1.0
+    assert g.count_nonzero().item() == 3
