@@ -31,7 +31,8 @@ namespace {
 
 constexpr int kMaxWidth = 8192;
 constexpr int kMaxParts = 256;         // backward workgroups: one per CU
-constexpr int kWaveRows = 4;           // rows side by side in a workgroup when a row is one wave's
+constexpr int kWaveRows = 4;           // forward: rows side by side when a row is one wave's
+constexpr int kBwdWaves = 8;           // backward: waves of a workgroup, two on every SIMD of its CU
 
 struct NormArgs {
     const void *X, *F, *gate;          // X: the residual stream (forward), Xn (backward)
@@ -48,22 +49,23 @@ struct NormArgs {
 // Sums of NV values over the lanes of a row: over a wave by exchanges; rows
 // of several waves add the waves' sums in order through one of two LDS
 // buffers in turn (a buffer is written again only after a barrier that every
-// reader of its last use has passed).
+// reader of its last use has passed).  Every thread of the workgroup calls it
+// equally often when a row has several waves.
 template <int NV>
 __device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[8][4], int &turn, int waves) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) v[i] = wave_sum(v[i]);
     if (waves == 1) return;
     static_assert(NV <= 4, "four sums at most");
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, w0 = w - w % waves;
     if (lane == 0)
 #pragma unroll
         for (int i = 0; i < NV; ++i) red[turn][w][i] = v[i];
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        float s = red[turn][0][i];
-        for (int x = 1; x < waves; ++x) s += red[turn][x][i];
+        float s = red[turn][w0][i];
+        for (int x = 1; x < waves; ++x) s += red[turn][w0 + x][i];
         v[i] = s;
     }
     turn ^= 1;
@@ -218,13 +220,48 @@ __global__ __launch_bounds__(512) void block_norm_fwd_kernel(NormArgs p) {
     }
 }
 
-// Sums over the tokens that the parameters' gradients need, kept in
-// registers over the rows of a workgroup: of y_F times T (times the token's
-// gate), of T alike, of dH times y_X and of dH; the second and the fourth
-// only with BIAS.  finish_kernel adds the workgroups' sums in order.
-template <class TS, class TA, int VEC, int CH, bool BIAS>
+// the rows of one token that the backward reads, as loaded; entries that the
+// lane does not own are zeros
+template <class TS, class TA, int VEC, int CH>
+struct BwdRows {
+    Pack<TS, VEC> x[CH], t[CH];
+    Pack<TA, VEC> h[CH], f[CH], g[CH];
+    __device__ __forceinline__ void load(const NormArgs &p, int64_t row, const Columns<VEC, CH> &k) {
+        const int64_t at = row * p.N;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            if (p.dXn) t[j].load(static_cast<const TS *>(p.dXn) + at + k.col[j]);
+            if (p.dH) {
+                x[j].load(static_cast<const TS *>(p.X) + at + k.col[j]);
+                h[j].load(static_cast<const TA *>(p.dH) + at + k.col[j]);
+            }
+            if (p.F) f[j].load(static_cast<const TA *>(p.F) + at + k.col[j]);
+            if (p.gate) g[j].load(static_cast<const TA *>(p.gate) + at + k.col[j]);
+        }
+    }
+    __device__ __forceinline__ void clear(const NormArgs &p, const Columns<VEC, CH> &k) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            if (k.skip[j] == 0) continue;
+            t[j].clear(k.skip[j]);
+            x[j].clear(k.skip[j]);
+            h[j].clear(k.skip[j]);
+            f[j].clear(k.skip[j]);
+        }
+    }
+};
+
+// Per token two rounds of sums over the row for RMS (squares of both rows and
+// sum(u x) at once, then the post-norm's), a third one ahead for the means of
+// LAYER; the next token's rows are on their way meanwhile.  The sums over the
+// tokens that the parameters' gradients need stay in registers over the rows
+// of a workgroup: of y_F times T (times the token's gate), of T alike, of dH
+// times y_X and of dH.  FULL: means and the sums for biases; without it (RMS
+// norms, no bias) a third of the arithmetic and half of the sums fall away.
+// block_norm_finish_kernel adds the workgroups' sums in order.
+template <class TS, class TA, int VEC, int CH, bool FULL>
 __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
-    constexpr int NE = VEC * CH, NS = BIAS ? 4 : 2;
+    constexpr int NE = VEC * CH, NS = FULL ? 4 : 2;
     __shared__ float red[2][8][4];
     extern __shared__ float share[];       // [rows][N] when rows > 1
     int turn = 0;
@@ -232,6 +269,8 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
     const int lane = int(threadIdx.x) % p.lpr;
     const Columns<VEC, CH> k(lane, p.lpr, p.N);
     const float inv_n = 1.f / float(p.N);
+    const bool pre_mean = FULL && p.dH && p.pre == COMERA_NORM_LAYER;
+    const bool post_mean = FULL && p.F && p.post == COMERA_NORM_LAYER;
     float pw[NE], w[NE], acc[NS][NE];
     load_param<VEC, CH>(p.gate_ch, 1.f, k, pw);
     {
@@ -245,78 +284,103 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
     for (int s = 0; s < NS; ++s)
 #pragma unroll
         for (int i = 0; i < NE; ++i) acc[s][i] = 0.f;
-    for (int64_t row = int64_t(blockIdx.x) * rows + int(threadIdx.x) / p.lpr; row < p.b;
-         row += int64_t(gridDim.x) * rows) {
+    // every thread takes equally many rows: those behind the last one read
+    // it again and write nothing
+    const int64_t step = int64_t(gridDim.x) * rows;
+    int64_t row = int64_t(blockIdx.x) * rows + int(threadIdx.x) / p.lpr;
+    BwdRows<TS, TA, VEC, CH> next;
+    next.load(p, min(row, p.b - 1), k);
+    for (int64_t base = int64_t(blockIdx.x) * rows; base < p.b; base += step, row += step) {
+        const bool live = row < p.b;
+        BwdRows<TS, TA, VEC, CH> in = next;
+        if (base + step < p.b) next.load(p, min(row + step, p.b - 1), k);
+        in.clear(p, k);
         const int64_t at = row * p.N;
-        float t[NE];
-        if (p.dXn) {
-            load_row<TS, VEC, CH>(p.dXn, at, k, t);
-        } else {
-#pragma unroll
-            for (int i = 0; i < NE; ++i) t[i] = 0.f;
-        }
-        if (p.dH) {
-            float x[NE], h[NE], mean, r;
-            load_row<TS, VEC, CH>(p.X, at, k, x);
-            load_row<TA, VEC, CH>(p.dH, at, k, h);
-            row_stats<VEC, CH>(x, k, p.pre, p.N, p.eps, red, turn, waves, mean, r);
-            float s[2] = {0.f, 0.f};
+        float x[NE], f[NE], t[NE];
+        float mean[2] = {0.f, 0.f};
+        if (FULL && (pre_mean || post_mean)) {
 #pragma unroll
             for (int i = 0; i < NE; ++i) {
-                x[i] = (x[i] - mean) * r;
-                acc[0 + NS / 2][i] += h[i] * x[i];
-                if constexpr (BIAS) acc[3][i] += h[i];
-                h[i] *= w[i];
-                s[0] += k.counts(i / VEC, i % VEC) ? h[i] * x[i] : 0.f;
-                s[1] += k.counts(i / VEC, i % VEC) ? h[i] : 0.f;
+                if (pre_mean) mean[0] += in.x[i / VEC].get(i % VEC);
+                if (post_mean) mean[1] += in.f[i / VEC].get(i % VEC);
             }
-            row_sum<2>(s, red, turn, waves);
-            const float sy = s[0] * inv_n, su = p.pre == COMERA_NORM_LAYER ? s[1] * inv_n : 0.f;
-#pragma unroll
-            for (int i = 0; i < NE; ++i) t[i] += r * (h[i] - su - x[i] * sy);
+            row_sum<2>(mean, red, turn, waves);
+            mean[0] *= inv_n;
+            mean[1] *= inv_n;
         }
-        if (p.dX) {
-            float x[NE];
-#pragma unroll
-            for (int i = 0; i < NE; ++i) x[i] = p.F ? p.a * t[i] : t[i];
-            store_row<TS, VEC, CH>(p.dX, at, k, x);
-        }
-        if (!p.F) continue;
-        float f[NE], mean = 0.f, r = 1.f;
-        load_row<TA, VEC, CH>(p.F, at, k, f);
-        if (p.post != COMERA_NORM_NONE) {
-            row_stats<VEC, CH>(f, k, p.post, p.N, p.eps, red, turn, waves, mean, r);
-#pragma unroll
-            for (int i = 0; i < NE; ++i) f[i] = (f[i] - mean) * r;
-        }
-        if (p.gate) {
-            float g[NE], z[NE], x[NE];
-            load_row<TA, VEC, CH>(p.gate, at, k, g);
-            load_param<VEC, CH>(p.post_w, 1.f, k, z);
-            load_param<VEC, CH>(p.post_b, 0.f, k, x);
-#pragma unroll
-            for (int i = 0; i < NE; ++i) {
-                z[i] = p.beta * t[i] * (f[i] * z[i] + x[i]);
-                t[i] *= g[i];
-            }
-            if (p.dgate) store_row<TA, VEC, CH>(p.dgate, at, k, z);
-        }
-        float s[2] = {0.f, 0.f};
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
-            acc[0][i] += t[i] * f[i];
-            if constexpr (BIAS) acc[1][i] += t[i];
+            const bool on = k.counts(i / VEC, i % VEC);
+            if (p.dH) {
+                x[i] = in.x[i / VEC].get(i % VEC);
+                if constexpr (FULL) x[i] = on ? x[i] - mean[0] : 0.f;
+                const float u = in.h[i / VEC].get(i % VEC) * w[i];
+                s[0] += x[i] * x[i];
+                s[1] += u * x[i];
+                if constexpr (FULL) s[2] += u;
+            }
+            if (p.F) {
+                f[i] = in.f[i / VEC].get(i % VEC);
+                if constexpr (FULL) f[i] = on ? f[i] - mean[1] : 0.f;
+                s[3] += f[i] * f[i];
+            }
+        }
+        if (p.dH || (p.F && p.post != COMERA_NORM_NONE)) row_sum<4>(s, red, turn, waves);
+#pragma unroll
+        for (int i = 0; i < NE; ++i) t[i] = p.dXn ? in.t[i / VEC].get(i % VEC) : 0.f;
+        if (p.dH) {
+            const float r = 1.f / sqrtf(s[0] * inv_n + p.eps);
+            const float sy = s[1] * r * inv_n, su = pre_mean ? s[2] * inv_n : 0.f;
+#pragma unroll
+            for (int i = 0; i < NE; ++i) {
+                const float h = live ? in.h[i / VEC].get(i % VEC) : 0.f, y = x[i] * r;
+                acc[NS / 2][i] += h * y;
+                if constexpr (FULL) acc[3][i] += h;
+                t[i] += r * (FULL ? h * w[i] - su - y * sy : h * w[i] - y * sy);
+            }
+        }
+        if (p.dX && live) {
+            float o[NE];
+#pragma unroll
+            for (int i = 0; i < NE; ++i) o[i] = p.F ? p.a * t[i] : t[i];
+            store_row<TS, VEC, CH>(p.dX, at, k, o);
+        }
+        if (!p.F) continue;
+        const float r = p.post != COMERA_NORM_NONE ? 1.f / sqrtf(s[3] * inv_n + p.eps) : 1.f;
+#pragma unroll
+        for (int i = 0; i < NE; ++i) f[i] *= r;
+        if (p.gate) {
+            float z[NE], o[NE];
+            load_param<VEC, CH>(p.post_w, 1.f, k, z);
+            load_param<VEC, CH>(p.post_b, 0.f, k, o);
+#pragma unroll
+            for (int i = 0; i < NE; ++i) {
+                z[i] = p.beta * t[i] * (f[i] * z[i] + o[i]);
+                t[i] *= in.g[i / VEC].get(i % VEC);
+            }
+            if (p.dgate && live) store_row<TA, VEC, CH>(p.dgate, at, k, z);
+        }
+        float q[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NE; ++i) {
+            // entries that are not the lane's own: f is zero, t need not be
+            const bool on = FULL ? k.counts(i / VEC, i % VEC) : true;
+            if (live) {
+                acc[0][i] += t[i] * f[i];
+                if constexpr (FULL) acc[1][i] += t[i];
+            }
             t[i] *= pw[i];
-            s[0] += k.counts(i / VEC, i % VEC) ? t[i] * f[i] : 0.f;
-            s[1] += k.counts(i / VEC, i % VEC) ? t[i] : 0.f;
+            q[0] += t[i] * f[i];
+            if constexpr (FULL) q[1] += on ? t[i] : 0.f;
         }
         if (p.post != COMERA_NORM_NONE) {
-            row_sum<2>(s, red, turn, waves);
-            const float sy = s[0] * inv_n, su = p.post == COMERA_NORM_LAYER ? s[1] * inv_n : 0.f;
+            row_sum<2>(q, red, turn, waves);
+            const float sy = q[0] * inv_n, su = post_mean ? q[1] * inv_n : 0.f;
 #pragma unroll
-            for (int i = 0; i < NE; ++i) t[i] = r * (t[i] - su - f[i] * sy);
+            for (int i = 0; i < NE; ++i) t[i] = r * (FULL ? t[i] - su - f[i] * sy : t[i] - f[i] * sy);
         }
-        if (p.dF) store_row<TA, VEC, CH>(p.dF, at, k, t);
+        if (p.dF && live) store_row<TA, VEC, CH>(p.dF, at, k, t);
     }
     if (!p.part) return;
     // the workgroup's sums: its rows added in order through LDS
@@ -332,7 +396,7 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
         for (int c = threadIdx.x; c < p.N; c += int(blockDim.x)) {
             float v = share[c];
             for (int x = 1; x < rows; ++x) v += share[x * p.N + c];
-            out[s * p.N + c] = v;
+            out[int64_t(s) * p.N + c] = v;
         }
         __syncthreads();
     }
@@ -340,37 +404,55 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
 
 struct FinishArgs {
     const float *part;
-    int parts, sums, N, post, token_gate;
+    int parts, N;
     const float *gate_ch, *post_w, *post_b;
     float beta;
     float *dgate, *dpost_w, *dpost_b, *dpre_w, *dpre_b;
 };
 
-constexpr int kFinCols = 16, kFinGroups = 16;
+constexpr int kFinCols = 32, kFinGroups = 32;
 
-// Sums of the workgroups' partials and the parameters' gradients from them.
-// 16 columns x 16 groups of partials per workgroup, the groups added in order.
+// Sums of the workgroups' partials and the parameters' gradients from them:
+// 32 columns x 32 groups of partials per workgroup (a thread has all its
+// loads in flight at once), the groups added in order.
+template <int NS>
 __global__ __launch_bounds__(kFinCols *kFinGroups) void block_norm_finish_kernel(FinishArgs a) {
-    __shared__ float red[4][kFinGroups][kFinCols];
+    constexpr int kPer = kMaxParts / kFinGroups;
+    __shared__ float red[NS][kFinGroups][kFinCols];
     const int l = threadIdx.x % kFinCols, g = threadIdx.x / kFinCols;
     const int c = blockIdx.x * kFinCols + l;
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (c < a.N)
-        for (int p = g; p < a.parts; p += kFinGroups)
-            for (int s = 0; s < a.sums; ++s) v[s] += a.part[(int64_t(p) * a.sums + s) * a.N + c];
-    for (int s = 0; s < 4; ++s) red[s][g][l] = v[s];
+    float v[NS], x[kPer][NS];
+    const int cc = min(c, a.N - 1);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int p = g + i * kFinGroups;
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+            x[i][s] = p < a.parts ? a.part[(int64_t(p) * NS + s) * a.N + cc] : 0.f;
+    }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        v[s] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) v[s] += x[i][s];
+        red[s][g][l] = v[s];
+    }
     __syncthreads();
-    if (g != 0 || c >= a.N) return;
-    for (int s = 0; s < 4; ++s)
-        for (int x = 1; x < kFinGroups; ++x) v[s] += red[s][x][l];
-    const float yT = v[0], T = a.sums == 4 ? v[1] : 0.f, yH = v[a.sums / 2], H = v[3];
+    if (g < NS) {                          // group s adds sum s ...
+        float sum = 0.f;
+        for (int i = 0; i < kFinGroups; ++i) sum += red[g][i][l];
+        red[g][0][l] = sum;                // read by this thread alone so far
+    }
+    __syncthreads();
+    if (g != 0 || c >= a.N) return;        // ... and group 0 forms the gradients
+    const float yT = red[0][0][l], T = NS == 4 ? red[1][0][l] : 0.f, yH = red[NS / 2][0][l];
     const float gate = a.gate_ch ? a.gate_ch[c] : 1.f;
     if (a.dpost_w) a.dpost_w[c] = a.beta * gate * yT;
     if (a.dpost_b) a.dpost_b[c] = a.beta * gate * T;
     if (a.dgate)
         a.dgate[c] = a.beta * (yT * (a.post_w ? a.post_w[c] : 1.f) + (a.post_b ? a.post_b[c] * T : 0.f));
     if (a.dpre_w) a.dpre_w[c] = yH;
-    if (a.dpre_b) a.dpre_b[c] = H;
+    if (NS == 4 && a.dpre_b) a.dpre_b[c] = red[NS - 1][0][l];
 }
 
 // ---------------------------------------------------------------- host side
@@ -390,28 +472,39 @@ bool norm_supported(const comera_block_norm_shape *s) {
 
 // How a row is spread: lanes per row and entries per lane.
 struct Spread {
-    int vec, ch, lpr;
-    int rows() const { return lpr == 64 ? kWaveRows : 1; }
-    int threads() const { return lpr == 64 ? 64 * kWaveRows : lpr; }
+    int vec, ch, lpr, rows;
+    int threads() const { return lpr * rows; }
 };
 
-// 8 entries a lane up to 512 columns; above, 12 or 16, whichever leaves fewer
-// idle lanes (768 columns: 64 lanes x 12); single entries below 8 columns
-Spread spread_of(int N) {
-    if (N < 8) return {1, 1, 64};
-    if (N <= 512) return {8, 1, 64};
+// Forward: 8 entries a lane up to 512 columns; above, 12 or 16, whichever
+// leaves fewer idle lanes (768 columns: 64 lanes x 12).  Single entries below
+// 8 columns.
+Spread fwd_spread(int N) {
+    if (N < 8) return {1, 1, 64, kWaveRows};
+    if (N <= 512) return {8, 1, 64, kWaveRows};
     const int l12 = (N + 767) / 768 * 64, l16 = (N + 1023) / 1024 * 64;
-    if (l12 * 12 < l16 * 16 && l12 <= 512) return {4, 3, l12};
-    return {8, 2, l16};
+    const Spread sp = l12 * 12 < l16 * 16 && l12 <= 512 ? Spread{4, 3, l12, 1} : Spread{8, 2, l16, 1};
+    return {sp.vec, sp.ch, sp.lpr, sp.lpr == 64 ? kWaveRows : 1};
+}
+
+// Backward: its registers hold two rows of four tensors and up to four sums,
+// so 8 entries a lane as long as eight waves cover the row (4096 columns),
+// 12 where one wave then does.
+Spread bwd_spread(int N) {
+    if (N < 8) return {1, 1, 64, kBwdWaves};
+    if (N > 512 && N <= 768) return {4, 3, 64, kBwdWaves};
+    if (N > 4096) return {8, 2, (N + 1023) / 1024 * 64, 1};
+    const int waves = (N + 511) / 512;
+    return {8, 1, 64 * waves, kBwdWaves / waves};
 }
 
 int64_t bwd_parts(const Spread &sp, int64_t b) {
-    return std::min<int64_t>((b + sp.rows() - 1) / sp.rows(), kMaxParts);
+    return std::min<int64_t>((b + sp.rows - 1) / sp.rows, kMaxParts);
 }
 
 template <class TS, class TA>
 void launch_fwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
-    const unsigned grid = unsigned(std::min<int64_t>((p.b + sp.rows() - 1) / sp.rows(), 4096));
+    const unsigned grid = unsigned(std::min<int64_t>((p.b + sp.rows - 1) / sp.rows, 4096));
     const dim3 block(sp.threads());
     if (sp.vec == 1)
         COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 1, 1>), dim3(grid), block, 0, st, p);
@@ -423,19 +516,19 @@ void launch_fwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
         COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 8, 2>), dim3(grid), block, 0, st, p);
 }
 
-template <class TS, class TA, bool BIAS>
+template <class TS, class TA, bool FULL>
 void launch_bwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
     const unsigned grid = unsigned(bwd_parts(sp, p.b));
     const dim3 block(sp.threads());
-    const size_t lds = sp.rows() > 1 ? sizeof(float) * sp.rows() * p.N : 0;
+    const size_t lds = sp.rows > 1 ? sizeof(float) * sp.rows * p.N : 0;
     if (sp.vec == 1)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 1, 1, BIAS>), dim3(grid), block, lds, st, p);
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 1, 1, FULL>), dim3(grid), block, lds, st, p);
     else if (sp.vec == 4)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 4, 3, BIAS>), dim3(grid), block, lds, st, p);
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 4, 3, FULL>), dim3(grid), block, lds, st, p);
     else if (sp.ch == 1)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 1, BIAS>), dim3(grid), block, lds, st, p);
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 1, FULL>), dim3(grid), block, lds, st, p);
     else
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 2, BIAS>), dim3(grid), block, lds, st, p);
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 2, FULL>), dim3(grid), block, lds, st, p);
 }
 
 }  // namespace
@@ -447,7 +540,7 @@ extern "C" {
 
 size_t comera_block_norm_workspace_bytes(const comera_block_norm_shape *s, int64_t b) {
     if (!norm_shape_ok(s) || !norm_supported(s) || b < 0) return 0;
-    return sizeof(float) * 4 * size_t(s->width) * size_t(std::max<int64_t>(1, bwd_parts(spread_of(int(s->width)), b)));
+    return sizeof(float) * 4 * size_t(s->width) * size_t(std::max<int64_t>(1, bwd_parts(bwd_spread(int(s->width)), b)));
 }
 
 comera_status comera_block_norm_forward(const comera_block_norm_shape *s, int64_t b, const void *X, const void *F,
@@ -481,7 +574,7 @@ comera_status comera_block_norm_forward(const comera_block_norm_shape *s, int64_
     p.eps = s->eps;
     p.a = s->res_scale;
     p.beta = s->branch_scale;
-    const Spread sp = spread_of(p.N);
+    const Spread sp = fwd_spread(p.N);
     p.lpr = sp.lpr;
     hipStream_t st = hipStream_t(stream);
     if (s->stream == COMERA_F32 && s->act == COMERA_F32)
@@ -507,15 +600,15 @@ comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64
         (!post && (post_w || post_b || dpost_w || dpost_b)) || (!pre && (pre_w || dpre_w || dpre_b || dH)))
         return COMERA_ERR_INVALID_ARG;
     const bool params = dpost_w || dpost_b || dpre_w || dpre_b || (channel && dgate);
-    const Spread sp = spread_of(int(s->width));
+    const Spread sp = bwd_spread(int(s->width));
     const int64_t parts = bwd_parts(sp, b);
     if (b > 0 && ((!dXn && !dH) || (dH && !Xn))) return COMERA_ERR_INVALID_ARG;
     if (params && b > 0 &&
         (!ws || ws_bytes < comera_block_norm_workspace_bytes(s, b) || reinterpret_cast<uintptr_t>(ws) % 8))
         return COMERA_ERR_WORKSPACE;
     hipStream_t st = hipStream_t(stream);
-    // the sums of T and of dH are formed only where a bias needs them
-    const bool bias = dpost_b || dpre_b || (channel && dgate && post_b);
+    const bool full = dpost_b || dpre_b || (channel && dgate && post_b) || s->pre == COMERA_NORM_LAYER ||
+                      s->post == COMERA_NORM_LAYER;
     NormArgs p{};
     p.X = Xn;
     p.F = F;
@@ -540,17 +633,16 @@ comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64
     p.lpr = sp.lpr;
     if (b > 0 && (params || dX || dF || p.dgate)) {
         if (s->stream == COMERA_F32 && s->act == COMERA_F32)
-            bias ? launch_bwd<float, float, true>(p, sp, st) : launch_bwd<float, float, false>(p, sp, st);
+            full ? launch_bwd<float, float, true>(p, sp, st) : launch_bwd<float, float, false>(p, sp, st);
         else if (s->stream == COMERA_F32)
-            bias ? launch_bwd<float, bf16, true>(p, sp, st) : launch_bwd<float, bf16, false>(p, sp, st);
+            full ? launch_bwd<float, bf16, true>(p, sp, st) : launch_bwd<float, bf16, false>(p, sp, st);
         else
-            bias ? launch_bwd<bf16, bf16, true>(p, sp, st) : launch_bwd<bf16, bf16, false>(p, sp, st);
+            full ? launch_bwd<bf16, bf16, true>(p, sp, st) : launch_bwd<bf16, bf16, false>(p, sp, st);
     }
     if (params) {
         FinishArgs f{};
         f.part = p.part;
         f.parts = int(parts);
-        f.sums = bias ? 4 : 2;
         f.N = p.N;
         f.gate_ch = p.gate_ch;
         f.post_w = post_w;
@@ -561,8 +653,11 @@ comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64
         f.dpost_b = dpost_b;
         f.dpre_w = dpre_w;
         f.dpre_b = dpre_b;
-        COMERA_LAUNCH(block_norm_finish_kernel, dim3(unsigned((p.N + kFinCols - 1) / kFinCols)),
-                      dim3(kFinCols * kFinGroups), 0, st, f);
+        const dim3 grid(unsigned((p.N + kFinCols - 1) / kFinCols)), block(kFinCols * kFinGroups);
+        if (full)
+            COMERA_LAUNCH((block_norm_finish_kernel<4>), grid, block, 0, st, f);
+        else
+            COMERA_LAUNCH((block_norm_finish_kernel<2>), grid, block, 0, st, f);
     }
     return note_hip(launch_status(), "block norm") ? COMERA_ERR_HIP : COMERA_OK;
 }

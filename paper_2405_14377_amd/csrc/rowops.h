@@ -62,6 +62,10 @@ struct Pack<float, V> {
         }
     }
     __device__ __forceinline__ float get(int i) const { return x[i]; }
+    __device__ __forceinline__ void clear(int first) {     // entries [0, first)
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = i < first ? 0.f : x[i];
+    }
     static __device__ __forceinline__ void store(float *p, const float (&v)[V]) {
         if constexpr (V % 4 == 0) {
 #pragma unroll
@@ -102,6 +106,11 @@ struct Pack<bf16, V> {
         }
     }
     __device__ __forceinline__ float get(int i) const { return i & 1 ? hi_bf16(x[i / 2]) : lo_bf16(x[i / 2]); }
+    __device__ __forceinline__ void clear(int first) {     // entries [0, first)
+#pragma unroll
+        for (int i = 0; i < V; i += 2)
+            x[i / 2] = i + 1 < first ? 0u : i < first ? x[i / 2] & 0xffff0000u : x[i / 2];
+    }
     static __device__ __forceinline__ void store(bf16 *p, const float (&v)[V]) {
         if constexpr (V % 8 == 0) {
 #pragma unroll
