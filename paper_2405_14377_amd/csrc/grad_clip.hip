@@ -35,7 +35,8 @@ struct GradChunk {
     const void *g[kChunkTensors];
     void *out[kChunkTensors];
     int64_t n[kChunkTensors];
-    uint32_t tile0[kChunkTensors + 1]; // first tile of each tensor
+    uint32_t tile0[kChunkTensors + 1]; // first tile of each tensor; behind the last one, the tiles and then 2^32 - 1
+    uint32_t tiles;
     uint64_t is_bf16[kChunkTensors / 64];
     int count;
     int part0, parts;                  // this launch's partials
@@ -43,17 +44,13 @@ struct GradChunk {
 };
 static_assert(sizeof(GradChunk) <= 3968, "the table is passed as a kernel argument");
 
-// tensor that holds tile t (the last one that starts at or before it)
+// tensor that holds tile t (the last one that starts at or before it): every
+// lane compares two entries of the table, so it takes one round trip
 __device__ __forceinline__ int tensor_of(const GradChunk &c, uint32_t t) {
-    int lo = 0, hi = c.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (c.tile0[mid] <= t)
-            lo = mid;
-        else
-            hi = mid - 1;
-    }
-    return lo;
+    static_assert(kChunkTensors == 128, "two entries a lane");
+    const int lane = threadIdx.x & 63;
+    const uint32_t x = c.tile0[lane], y = c.tile0[64 + lane];
+    return __popcll(__ballot(x <= t)) + __popcll(__ballot(y <= t)) - 1;
 }
 
 // sum over a workgroup of 256 threads in a fixed order, in every thread
@@ -67,35 +64,61 @@ __device__ __forceinline__ double block_sum(double v) {
     return v;
 }
 
+// One tile: each thread's 16-byte pieces, all in flight at once.  use(p, i) is
+// called for every whole piece at entry i, rest(j) for the entries behind the
+// last one.
+template <class T, class Use, class Rest>
+__device__ __forceinline__ void for_tile(const T *g, int64_t at, int64_t n, Use use, Rest rest) {
+    constexpr int V = 16 / sizeof(T), U = kTile / (V * kGradThreads);
+    const int64_t i0 = at + int64_t(threadIdx.x) * V;
+    if (at + kTile <= n) {
+        Pack<T, V> p[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) p[u].load(g + i0 + u * kGradThreads * V);
+#pragma unroll
+        for (int u = 0; u < U; ++u) use(p[u], i0 + u * kGradThreads * V);
+        return;
+    }
+    // the last tile of a tensor: pieces behind its last whole one read that
+    // one (or nothing) and are not used
+    const int64_t whole = at + (n - at) / V * V;
+    if (whole > at) {
+        Pack<T, V> p[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) p[u].load(g + min(i0 + u * kGradThreads * V, whole - V));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i0 + u * kGradThreads * V < whole) use(p[u], i0 + u * kGradThreads * V);
+    }
+    if (whole + threadIdx.x < n) rest(whole + threadIdx.x);
+}
+
 template <class T>
 __device__ __forceinline__ double tile_squares(const T *g, int64_t at, int64_t n) {
     constexpr int V = 16 / sizeof(T);
-    double s = 0;
-    const int64_t end = min(n, at + kTile);
-    for (int64_t i = at + int64_t(threadIdx.x) * V; i < end; i += kGradThreads * V) {
-        if (i + V <= end) {
-            Pack<T, V> p;
-            p.load(g + i);
+    double s[2] = {0, 0};
+    auto add = [&](float x, int k) { s[k & 1] += double(x) * double(x); };
+    for_tile<T>(
+        g, at, n,
+        [&](const Pack<T, V> &p, int64_t) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) s += double(p.get(e)) * double(p.get(e));
-        } else {
-            for (int64_t j = i; j < end; ++j) {
-                Pack<T, 1> p;
-                p.load(g + j);
-                s += double(p.get(0)) * double(p.get(0));
-            }
-        }
-    }
-    return s;
+            for (int e = 0; e < V; ++e) add(p.get(e), e);
+        },
+        [&](int64_t j) {
+            Pack<T, 1> p;
+            p.load(g + j);
+            add(p.get(0), 0);
+        });
+    return s[0] + s[1];
 }
 
 __global__ __launch_bounds__(kGradThreads) void grad_squares_kernel(GradChunk c, double *part) {
-    const uint32_t tiles = c.tile0[c.count];
-    const uint32_t t0 = uint32_t(uint64_t(tiles) * blockIdx.x / c.parts);
-    const uint32_t t1 = uint32_t(uint64_t(tiles) * (blockIdx.x + 1) / c.parts);
+    const uint32_t t0 = uint32_t(uint64_t(c.tiles) * blockIdx.x / c.parts);
+    const uint32_t t1 = uint32_t(uint64_t(c.tiles) * (blockIdx.x + 1) / c.parts);
     double s = 0;
+    int i = tensor_of(c, t0);
     for (uint32_t t = t0; t < t1; ++t) {
-        const int i = tensor_of(c, t);
+        while (t >= c.tile0[i + 1]) ++i;
         const int64_t at = int64_t(t - c.tile0[i]) * kTile;
         s += (c.is_bf16[i >> 6] >> (i & 63)) & 1 ? tile_squares(static_cast<const bf16 *>(c.g[i]), at, c.n[i])
                                                  : tile_squares(static_cast<const float *>(c.g[i]), at, c.n[i]);
@@ -126,24 +149,20 @@ __global__ __launch_bounds__(kGradThreads) void grad_norm_kernel(const double *p
 template <class T>
 __device__ __forceinline__ void tile_scale(const T *g, T *out, int64_t at, int64_t n, float c) {
     constexpr int V = 16 / sizeof(T);
-    const int64_t end = min(n, at + kTile);
-    for (int64_t i = at + int64_t(threadIdx.x) * V; i < end; i += kGradThreads * V) {
-        if (i + V <= end) {
-            Pack<T, V> p;
-            p.load(g + i);
+    for_tile<T>(
+        g, at, n,
+        [&](const Pack<T, V> &p, int64_t i) {
             float v[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) v[e] = c * p.get(e);
             Pack<T, V>::store(out + i, v);
-        } else {
-            for (int64_t j = i; j < end; ++j) {
-                Pack<T, 1> p;
-                p.load(g + j);
-                const float v[1] = {c * p.get(0)};
-                Pack<T, 1>::store(out + j, v);
-            }
-        }
-    }
+        },
+        [&](int64_t j) {
+            Pack<T, 1> p;
+            p.load(g + j);
+            const float v[1] = {c * p.get(0)};
+            Pack<T, 1>::store(out + j, v);
+        });
 }
 
 __global__ __launch_bounds__(kGradThreads) void grad_scale_kernel(GradChunk c, const double *part, float scale,
@@ -152,11 +171,13 @@ __global__ __launch_bounds__(kGradThreads) void grad_scale_kernel(GradChunk c, c
     if (c.part0 == 0 && blockIdx.x == 0 && threadIdx.x == 0) write_norm(v, norm, flag);
     const bool clip = isfinite(float(v)) && v > double(max_norm);
     const float f = clip ? float(double(scale) * (double(max_norm) / v)) : scale;
-    const uint32_t tiles = c.tile0[c.count];
     // from the last tile back: what the first pass read last is still cached
-    for (uint32_t k = blockIdx.x; k < tiles; k += gridDim.x) {
-        const uint32_t t = tiles - 1 - k;
-        const int i = tensor_of(c, t);
+    const uint32_t b = gridDim.x - 1 - blockIdx.x;
+    const uint32_t t0 = uint32_t(uint64_t(c.tiles) * b / gridDim.x);
+    const uint32_t t1 = uint32_t(uint64_t(c.tiles) * (b + 1) / gridDim.x);
+    int i = tensor_of(c, t1 - 1);
+    for (uint32_t t = t1; t-- > t0;) {
+        while (t < c.tile0[i]) --i;
         if (f == 1.f && c.out[i] == c.g[i]) continue;
         const int64_t at = int64_t(t - c.tile0[i]) * kTile;
         if ((c.is_bf16[i >> 6] >> (i & 63)) & 1)
@@ -219,7 +240,10 @@ comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count,
             for (int64_t i = 0; i < count; ++i) {
                 const comera_grad_tensor &t = tensors[i];
                 if (t.n == 0) continue;
-                if (p->chunks.empty() || p->chunks.back().count == kChunkTensors) p->chunks.emplace_back();
+                if (p->chunks.empty() || p->chunks.back().count == kChunkTensors) {
+                    p->chunks.emplace_back();
+                    std::fill(p->chunks.back().tile0 + 1, p->chunks.back().tile0 + kChunkTensors + 1, 0xffffffffu);
+                }
                 GradChunk &c = p->chunks.back();
                 const int k = c.count++;
                 c.g[k] = t.g;
@@ -229,7 +253,8 @@ comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count,
                 if (t.dtype == COMERA_BF16) c.is_bf16[k >> 6] |= uint64_t(1) << (k & 63);
             }
             for (GradChunk &c : p->chunks) {
-                const int64_t n = c.tile0[c.count];
+                c.tiles = c.tile0[c.count];
+                const int64_t n = c.tiles;
                 c.part0 = p->parts;
                 c.parts = int(std::max<int64_t>(1, std::min<int64_t>(n, int64_t(double(n) / tiles * kGradParts))));
                 p->parts += c.parts;
@@ -284,7 +309,7 @@ comera_status comera_grad_clip(comera_grad_plan_t p, float scale, float max_norm
     for (const GradChunk &c : p->chunks)
         COMERA_LAUNCH(grad_squares_kernel, dim3(unsigned(c.parts)), dim3(kGradThreads), 0, st, c, part);
     for (const GradChunk &c : p->chunks)
-        COMERA_LAUNCH(grad_scale_kernel, dim3(std::min<unsigned>(c.tile0[c.count], kScaleBlocks)), dim3(kGradThreads),
+        COMERA_LAUNCH(grad_scale_kernel, dim3(std::min<unsigned>(c.tiles, kScaleBlocks)), dim3(kGradThreads),
                       0, st, c, part, scale, max_norm, norm, flag);
     return note_hip(launch_status(), "gradient clipping") ? COMERA_ERR_HIP : COMERA_OK;
 }
