@@ -62,12 +62,12 @@ __device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[8][4], int 
 #pragma unroll
         for (int i = 0; i < NV; ++i) red[turn][w][i] = v[i];
     __syncthreads();
+    // eight lanes read the eight waves' sums at once and exchange them
+    const int x = lane & 7;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        float s = red[turn][w0][i];
-        for (int x = 1; x < waves; ++x) s += red[turn][w0 + x][i];
-        v[i] = s;
-    }
+    for (int i = 0; i < NV; ++i) v[i] = red[turn][min(w0 + x, 7)][i];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = sum_of_8(x < waves ? v[i] : 0.f);
     turn ^= 1;
 }
 
@@ -167,7 +167,7 @@ __device__ __forceinline__ void row_stats(const float (&v)[CH * VEC], const Colu
 template <class TS, class TA, int VEC, int CH>
 __global__ __launch_bounds__(512) void block_norm_fwd_kernel(NormArgs p) {
     constexpr int NE = VEC * CH;
-    __shared__ float red[2][8][4];
+    __shared__ __attribute__((aligned(16))) float red[2][8][4];
     int turn = 0;
     const int waves = p.lpr >> 6, rows = int(blockDim.x) / p.lpr;
     const int lane = int(threadIdx.x) % p.lpr;
@@ -262,7 +262,8 @@ struct BwdRows {
 template <class TS, class TA, int VEC, int CH, bool FULL>
 __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
     constexpr int NE = VEC * CH, NS = FULL ? 4 : 2;
-    __shared__ float red[2][8][4];
+    constexpr bool AHEAD = NE <= 12;       // with 16 entries a lane two tokens' rows do not fit the registers
+    __shared__ __attribute__((aligned(16))) float red[2][8][4];
     extern __shared__ float share[];       // [rows][N] when rows > 1
     int turn = 0;
     const int waves = p.lpr >> 6, rows = int(blockDim.x) / p.lpr;
@@ -289,11 +290,16 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
     const int64_t step = int64_t(gridDim.x) * rows;
     int64_t row = int64_t(blockIdx.x) * rows + int(threadIdx.x) / p.lpr;
     BwdRows<TS, TA, VEC, CH> next;
-    next.load(p, min(row, p.b - 1), k);
+    if constexpr (AHEAD) next.load(p, min(row, p.b - 1), k);
     for (int64_t base = int64_t(blockIdx.x) * rows; base < p.b; base += step, row += step) {
         const bool live = row < p.b;
-        BwdRows<TS, TA, VEC, CH> in = next;
-        if (base + step < p.b) next.load(p, min(row + step, p.b - 1), k);
+        BwdRows<TS, TA, VEC, CH> in;
+        if constexpr (AHEAD) {
+            in = next;
+            if (base + step < p.b) next.load(p, min(row + step, p.b - 1), k);
+        } else {
+            in.load(p, min(row, p.b - 1), k);
+        }
         in.clear(p, k);
         const int64_t at = row * p.N;
         float x[NE], f[NE], t[NE];
@@ -488,12 +494,15 @@ Spread fwd_spread(int N) {
 }
 
 // Backward: its registers hold two rows of four tensors and up to four sums,
-// so 8 entries a lane as long as eight waves cover the row (4096 columns),
-// 12 where one wave then does.
+// so 8 entries a lane as long as eight waves cover the row (4096 columns), 12
+// where one wave then does (up to 768) or eight waves do (up to 6144), and 16
+// above, which read one row at a time: 2048 x 5000 LAYER fp32 with 16 entries
+// and two rows spilled registers (165 us; 54 with 12).
 Spread bwd_spread(int N) {
     if (N < 8) return {1, 1, 64, kBwdWaves};
     if (N > 512 && N <= 768) return {4, 3, 64, kBwdWaves};
-    if (N > 4096) return {8, 2, (N + 1023) / 1024 * 64, 1};
+    if (N > 6144) return {8, 2, (N + 1023) / 1024 * 64, 1};
+    if (N > 4096) return {4, 3, (N + 767) / 768 * 64, 1};
     const int waves = (N + 511) / 512;
     return {8, 1, 64 * waves, kBwdWaves / waves};
 }

@@ -134,21 +134,29 @@ struct Pack<bf16, V> {
     }
 };
 
+// v of the lane that the DPP control `ctrl` names, in the rows of 16 lanes
+// that `rows` names; 0 in the other rows
+template <int ctrl, int rows>
+__device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float(
+        uint32_t(__builtin_amdgcn_update_dpp(0, int(__float_as_uint(v)), ctrl, rows, 0xf, rows == 0xf)));
+}
+
+// sum over 8 lanes in a row, the same bits in each of them
+__device__ __forceinline__ float sum_of_8(float v) {
+    v += dpp<0xb1, 0xf>(v);      // quad_perm 1,0,3,2
+    v += dpp<0x4e, 0xf>(v);      // quad_perm 2,3,0,1
+    v += dpp<0x141, 0xf>(v);     // row_half_mirror
+    return v;
+}
+
 // Sum over the 64 lanes of a wave, the same bits in every lane: exchanges
 // within 16 lanes, then the row totals are passed up to lane 63.
 __device__ __forceinline__ float wave_sum(float v) {
-    auto dpp = [](float x, auto ctrl, auto rows) {
-        return __uint_as_float(
-            uint32_t(__builtin_amdgcn_update_dpp(0, int(__float_as_uint(x)), ctrl.value, rows.value, 0xf, false)));
-    };
-    using std::integral_constant;
-    const integral_constant<int, 0xf> all{};
-    v += dpp(v, integral_constant<int, 0xb1>{}, all);      // quad_perm 1,0,3,2
-    v += dpp(v, integral_constant<int, 0x4e>{}, all);      // quad_perm 2,3,0,1
-    v += dpp(v, integral_constant<int, 0x141>{}, all);     // row_half_mirror
-    v += dpp(v, integral_constant<int, 0x140>{}, all);     // row_mirror
-    v += dpp(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});   // row_bcast:15
-    v += dpp(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});   // row_bcast:31
+    v = sum_of_8(v);
+    v += dpp<0x140, 0xf>(v);     // row_mirror
+    v += dpp<0x142, 0xa>(v);     // row_bcast:15
+    v += dpp<0x143, 0xc>(v);     // row_bcast:31
     return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), 63)));
 }
 
