@@ -59,34 +59,83 @@ constexpr int kGroupThreads = 64 * kGroupWaves;
 constexpr int kGroupBits = 9;
 constexpr int kGroupQ = 1 << kGroupBits;   // most ids of one workgroup: 32 KiB of counters
 constexpr int kGroupUnroll = 8;        // ids in flight per lane
-constexpr int kGroupList = 160;        // owned tokens that a wave keeps: 20 KiB
+constexpr int kGroupList = 192;        // owned tokens that a wave keeps: 24 KiB
 constexpr int kGroupStep = 64 * kGroupUnroll;
 
 struct GroupArgs {
     const int64_t *ids;
-    int64_t n, V, pad;
+    int64_t n, V;
+    uint32_t pad;       // 2^32 - 1: none
     int lg, Q;
+    uint32_t few;       // an id with more tokens goes to the list of long ones
     uint2 *order;       // (token, id) by id
     uint2 *range;       // (first place, tokens) of each id
+    uint32_t *many;     // [workgroup][Q] its long ids
+    uint32_t *n_many;   // [workgroup] how many
     uint32_t *total;    // tokens with an id
     int32_t *err_flag;
 };
 
-// one step of a wave's walk over its tokens: kGroupUnroll ids a lane
-__device__ __forceinline__ void load_ids(const GroupArgs &a, int64_t b, int64_t s1, int lane,
-                                         int64_t (&id)[kGroupUnroll]) {
+constexpr uint32_t kNoId = 0xffffffffu;
+
+// one step of a wave's walk over its tokens: kGroupUnroll ids a lane (b is
+// uniform; behind the last token the last id is read again)
+__device__ __forceinline__ void load_ids(const GroupArgs &a, int64_t b, uint32_t lane, int64_t (&id)[kGroupUnroll]) {
+    if (b + kGroupStep <= a.n) {
+        const int64_t *p = a.ids + b;
 #pragma unroll
-    for (int u = 0; u < kGroupUnroll; ++u) {
-        const int64_t at = b + u * 64 + lane;
-        id[u] = a.ids[min(at, s1 - 1)];
+        for (int u = 0; u < kGroupUnroll; ++u) id[u] = p[u * 64 + lane];
+    } else {
+#pragma unroll
+        for (int u = 0; u < kGroupUnroll; ++u) id[u] = a.ids[min(b + u * 64 + lane, a.n - 1)];
     }
+}
+
+// the id, or kNoId for padding and ids out of range
+__device__ __forceinline__ uint32_t good_id(const GroupArgs &a, int64_t id) {
+    const uint32_t x = uint64_t(id) < uint64_t(a.V) ? uint32_t(id) : kNoId;
+    return x == a.pad ? kNoId : x;
+}
+
+// Walks the tokens [s0, s1) of a wave; take(own, m, token, id) is called for
+// every 64 tokens of which some lanes (m) hold ids of workgroup g.  Returns
+// the number of tokens of the workgroups before it.
+template <class Take>
+__device__ __forceinline__ uint32_t walk(const GroupArgs &a, int64_t s0, int64_t s1, uint32_t lane, uint32_t g,
+                                         Take take) {
+    const uint32_t mask = (1u << a.lg) - 1;
+    uint32_t below = 0;
+    int64_t next[kGroupUnroll];
+    if (s0 < s1) load_ids(a, s0, lane, next);
+    for (int64_t b = s0; b < s1; b += kGroupStep) {
+        uint32_t id[kGroupUnroll];
+#pragma unroll
+        for (int u = 0; u < kGroupUnroll; ++u) id[u] = good_id(a, next[u]);
+        if (b + kGroupStep > a.n) {
+#pragma unroll
+            for (int u = 0; u < kGroupUnroll; ++u)
+                if (b + u * 64 + lane >= a.n) id[u] = kNoId;
+        }
+        if (b + kGroupStep < s1) load_ids(a, b + kGroupStep, lane, next);
+#pragma unroll
+        for (int u = 0; u < kGroupUnroll; ++u) {
+            const uint32_t k = id[u] & mask;           // kNoId: the last workgroup's, and below none
+            below += uint32_t(__popcll(__ballot(k < g)));
+            if (__ballot(k == g)) {
+                const bool own = k == g && id[u] != kNoId;
+                take(own, __ballot(own), uint32_t(b + u * 64 + lane), id[u]);
+            }
+        }
+    }
+    return below;
 }
 
 // Puts 64 owned tokens (those lanes with `own`) to their places: lanes of one
 // id are ranked by their lane number, their first lane moves the id's place
 // on.  Every id bit halves the set of lanes that agree with this one.
-__device__ __forceinline__ void put_tokens(const GroupArgs &a, volatile uint32_t *place, bool own, uint32_t token,
-                                           uint32_t q, uint32_t id, int lane) {
+__device__ __forceinline__ void put_tokens(const GroupArgs &a, volatile uint32_t *place, bool own, uint64_t token_id,
+                                           uint32_t lane) {
+    const uint32_t q = uint32_t(token_id) >> a.lg;
     uint64_t same = __ballot(own);
 #pragma unroll
     for (int b = 0; b < kGroupBits; ++b) {
@@ -96,8 +145,17 @@ __device__ __forceinline__ void put_tokens(const GroupArgs &a, volatile uint32_t
     if (own) {
         const uint32_t rank = uint32_t(__popcll(same & ((uint64_t(1) << lane) - 1)));
         const uint32_t first = place[q];
-        a.order[first + rank] = make_uint2(token, id);
+        a.order[first + rank] = make_uint2(uint32_t(token_id >> 32), uint32_t(token_id));
         if (rank == 0) place[q] = first + uint32_t(__popcll(same));
+    }
+}
+
+// the first `n` tokens of a wave's list
+__device__ __forceinline__ void put_list(const GroupArgs &a, volatile uint32_t *place, const volatile uint64_t *list,
+                                         uint32_t n, uint32_t lane) {
+    for (uint32_t i = 0; i < n; i += 64) {
+        const bool own = i + lane < n;
+        put_tokens(a, place, own, own ? list[i + lane] : 0, lane);
     }
 }
 
@@ -109,47 +167,35 @@ __device__ __forceinline__ void put_tokens(const GroupArgs &a, volatile uint32_t
 // counters, lists the owned tokens, and counts the tokens of lower
 // workgroups, which end where this one's begin.  A prefix sum over (id, wave)
 // turns the counters into places, and the lists, in the order of the walk, go
-// to them; a wave that owns more tokens than its list holds walks its part
-// again.  Bound by the latency and the L2 reads of the ids, 8 n bytes by each
-// of 256 CUs.
+// to them; a wave that owns more tokens than its list holds (an id that is a
+// good part of the batch) walks its part again, list by list.  Bound by the
+// instructions of the walk, about 10 per 64 ids and wave in each of 256 CUs.
 __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a) {
     extern __shared__ uint32_t cnt[];                  // [kGroupWaves][Q]
-    __shared__ uint32_t wsum[kGroupWaves], wbelow[kGroupWaves];
-    __shared__ uint2 list[kGroupWaves][kGroupList];    // (token, id)
-    const int t = threadIdx.x, w = t >> 6, lane = t & 63, Q = a.Q;
-    const uint32_t g = blockIdx.x, mask = (1u << a.lg) - 1;
+    __shared__ uint32_t wsum[kGroupWaves], wbelow[kGroupWaves], longs;
+    __shared__ uint64_t lists[kGroupWaves][kGroupList];            // token << 32 | id
+    const int t = threadIdx.x, w = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, Q = a.Q;
+    const uint32_t g = blockIdx.x;
     for (int i = t; i < kGroupWaves * Q; i += kGroupThreads) cnt[i] = 0;
+    if (t == 0) longs = 0;
     __syncthreads();
     const int64_t seg = ((a.n + kGroupWaves - 1) / kGroupWaves + kGroupStep - 1) / kGroupStep * kGroupStep;
     const int64_t s0 = w * seg, s1 = min(a.n, s0 + seg);
-    uint32_t below = 0, listed = 0;
-    bool bad = false;
-    for (int64_t b = s0; b < s1; b += kGroupStep) {
-        int64_t id[kGroupUnroll];
-        load_ids(a, b, s1, lane, id);
-#pragma unroll
-        for (int u = 0; u < kGroupUnroll; ++u) {
-            const int64_t at = b + u * 64 + lane;
-            const bool in = uint64_t(id[u]) < uint64_t(a.V);
-            const bool here = at < s1;
-            bad = bad || !in;                          // lanes behind the end repeat an id
-            const uint32_t k = uint32_t(id[u]) & mask;
-            const bool counts = here && in && id[u] != a.pad;
-            below += counts && k < g ? 1 : 0;
-            const bool own = counts && k == g;
-            const uint64_t m = __ballot(own);
-            if (m) {
-                if (own) {
-                    atomicAdd(&cnt[w * Q + int(uint32_t(id[u]) >> a.lg)], 1u);
-                    const uint32_t i = listed + uint32_t(__popcll(m & ((uint64_t(1) << lane) - 1)));
-                    if (i < kGroupList) list[w][i] = make_uint2(uint32_t(at), uint32_t(id[u]));
-                }
-                listed += uint32_t(__popcll(m));
-            }
-        }
-    }
-    if (g == 0 && bad && a.err_flag) *a.err_flag = 1;
-    for (int o = 32; o; o >>= 1) below += __shfl_xor(below, o);
+    volatile uint64_t *list = lists[w];
+    uint32_t listed = 0;
+    auto append = [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
+        const uint32_t i = listed + uint32_t(__popcll(m & ((uint64_t(1) << lane) - 1)));
+        if (own && i < kGroupList) list[i] = uint64_t(token) << 32 | id;
+        listed += uint32_t(__popcll(m));
+    };
+    const uint32_t below = walk(a, s0, s1, lane, g, [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
+        if (own) atomicAdd(&cnt[w * Q + int(id >> a.lg)], 1u);
+        append(own, m, token, id);
+    });
+    // ids out of range: every workgroup looks at its share of the tokens
+    if (a.err_flag)
+        for (int64_t at = int64_t(g) * kGroupThreads + t; at < a.n; at += int64_t(gridDim.x) * kGroupThreads)
+            if (uint64_t(a.ids[at]) >= uint64_t(a.V)) *a.err_flag = 1;
     if (lane == 0) wbelow[w] = below;
     __syncthreads();
     // thread q < Q owns one id: its total, and those of the ids before it
@@ -171,6 +217,7 @@ __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a)
     if (t < Q) {
         const int64_t id = (int64_t(t) << a.lg) + g;
         if (id < a.V) a.range[id] = make_uint2(base, mine);
+        if (mine > a.few) a.many[int64_t(g) * Q + atomicAdd(&longs, 1u)] = uint32_t(id);   // in any order
         for (int x = 0; x < kGroupWaves; ++x) {
             const uint32_t c = cnt[x * Q + t];
             cnt[x * Q + t] = base;
@@ -180,90 +227,100 @@ __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a)
     // all tokens with an id end behind the last id of the last workgroup
     if (g == gridDim.x - 1 && t == kGroupThreads - 1) *a.total = base;
     __syncthreads();
+    if (t == 0) a.n_many[g] = longs;
     volatile uint32_t *place = cnt + w * Q;            // this wave's places
     if (listed <= kGroupList) {
-        for (uint32_t i0 = 0; i0 < listed; i0 += 64) {
-            const bool own = i0 + lane < listed;
-            const uint2 x = list[w][own ? i0 + lane : 0];
-            put_tokens(a, place, own, x.x, x.y >> a.lg, x.y, lane);
-        }
+        put_list(a, place, list, listed, lane);
         return;
     }
-    for (int64_t b = s0; b < s1; b += kGroupStep) {
-        int64_t id[kGroupUnroll];
-        load_ids(a, b, s1, lane, id);
-#pragma unroll 1
-        for (int u = 0; u < kGroupUnroll; ++u) {
-            int64_t x = id[0];
-#pragma unroll
-            for (int k = 1; k < kGroupUnroll; ++k) x = u == k ? id[k] : x;
-            const int64_t at = b + u * 64 + lane;
-            const uint32_t i = uint32_t(x);
-            const bool own = at < s1 && uint64_t(x) < uint64_t(a.V) && x != a.pad && (i & mask) == g;
-            if (__ballot(own)) put_tokens(a, place, own, uint32_t(at), i >> a.lg, i, lane);
+    listed = 0;
+    walk(a, s0, s1, lane, g, [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
+        append(own, m, token, id);
+        if (listed > kGroupList - 64) {
+            put_list(a, place, list, listed, lane);
+            listed = 0;
         }
-    }
+    });
+    put_list(a, place, list, listed, lane);
 }
 
 // ---------------------------------------------------------------- sums by id
-// Column slice of a wave: 64 lanes x VEC columns.  The last lane with columns
-// is moved back to end at the row's end, as in the forward.
-constexpr int kSumVec = 4;
+constexpr int kSumVec = 4;             // columns of a lane
 constexpr int kSumLoads = 16;          // rows in flight per wave
+constexpr int kFillIds = 64;           // ids of one workgroup that writes zeros
 
-// One wave adds the rows of C consecutive places of the order, one column
-// slice of them, in order.  An id whose places all lie in the chunk gets its
-// row of dT; what an id has here that goes on in the next chunk goes to
-// last[chunk], what came from the chunk before (and perhaps goes on) to
-// first[chunk], fp32 and unscaled, for dense_finish_kernel.  Chunks of equal
-// length keep every wave busy alike however the ids are distributed.
+struct SumArgs {
+    const void *dY;
+    int64_t V, E;
+    int slices;         // column slices of a row: 64 lanes x VEC columns
+    int lgC;            // log2 of the places of one chunk
+    uint32_t few;       // tokens of an id that one wave adds alone
+    float scale;
+    const uint2 *order, *range;
+    const uint32_t *many, *n_many, *total;
+    int Q;
+    float *first, *last;
+    void *dT;
+    uint32_t sum_blocks;               // of the grid's workgroups, the ones that add
+};
+
+// One wave adds, in order, one column slice of the rows of the ids that begin
+// in C consecutive places of the order.  An id of at most `few` tokens is
+// added to its end, also behind the chunk's end (which 64 lanes, one place
+// each, reach); an id of more tokens is cut at the chunks' ends and leaves
+// fp32 unscaled partials, last[chunk] where it begins and first[chunk] where
+// it goes on, for dense_finish_kernel.  Chunks of equal length keep every
+// wave busy alike however the ids are distributed.
 template <class TY, class TT, int VEC>
-__device__ __forceinline__ void sum_chunk(const TY *dY, int64_t E, int64_t chunk, int slice, int C, uint32_t nv,
-                                          float scale, const uint2 *order, TT *dT, float *first, float *last) {
-    const int lane = threadIdx.x & 63;
-    const int64_t p0 = chunk * C;
-    const int cnt = int(min(int64_t(C), int64_t(nv) - p0));
-    // entry p0 - 1 + lane: the chunk's places and one on either side
-    uint2 me = make_uint2(0, 0xffffffffu);             // an id that no place has
-    const int64_t at = p0 - 1 + lane;
-    if (at >= 0 && at < nv && lane <= C + 1) me = order[at];
-    const int64_t c0 = int64_t(slice) * (64 * VEC) + lane * VEC;
+__device__ __forceinline__ void sum_chunk(const SumArgs &a, int64_t chunk, int slice, uint32_t nv) {
+    const int lane = threadIdx.x & 63, C = 1 << a.lgC;
+    const int64_t E = a.E, p0 = chunk << a.lgC, c0 = int64_t(slice) * (64 * VEC) + lane * VEC;
     const bool on = c0 < E;
     const int64_t c = on ? min(c0, E - VEC) : 0;
-    const uint32_t next = __shfl_down(me.y, 1);
-    const uint64_t ends = __ballot(lane >= 1 && lane <= cnt && me.y != next) >> 1;   // bit k: place k is its id's last
-    const bool goes_in = __builtin_amdgcn_readlane(int(me.y), 0) == __builtin_amdgcn_readlane(int(me.y), 1);
+    const bool here = p0 + lane < nv;
+    const uint2 me = here ? a.order[p0 + lane] : make_uint2(0, 0);
+    const uint2 rg = here ? a.range[me.y] : make_uint2(0, 0);
+    const uint32_t pos = uint32_t(p0) + lane;
+    const bool few = rg.y <= a.few;
+    const bool mine = here && (few ? rg.x >= uint32_t(p0) && rg.x < uint32_t(p0) + C : lane < C);
+    const uint64_t todo = __ballot(mine);
+    if (!todo) return;
+    const int k1 = 64 - __clzll((long long)todo);
+    int k0 = __ffsll((unsigned long long)todo) - 1;    // the places of one run of lanes
+    const bool ends = pos + 1 == rg.x + rg.y;
+    const uint64_t cut = __ballot(mine && (ends || (!few && lane == C - 1)));
+    const uint64_t whole = __ballot(few);
+    const uint64_t begun = __ballot(rg.x >= uint32_t(p0));         // the id begins in this chunk
+    const TY *dY = static_cast<const TY *>(a.dY);
     float acc[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-    bool from_before = goes_in;
-    for (int k0 = 0; k0 < cnt; k0 += kSumLoads) {
+    for (; k0 < k1; k0 += kSumLoads) {
         Pack<TY, VEC> x[kSumLoads];
 #pragma unroll
         for (int k = 0; k < kSumLoads; ++k) {
-            // places behind the chunk's end read its last row again
-            const uint32_t tok = uint32_t(__builtin_amdgcn_readlane(int(me.x), 1 + min(k0 + k, cnt - 1)));
+            // places behind the last one read its row again
+            const uint32_t tok = uint32_t(__builtin_amdgcn_readlane(int(me.x), min(k0 + k, k1 - 1)));
             x[k].load(dY + int64_t(tok) * E + c);
         }
 #pragma unroll
         for (int k = 0; k < kSumLoads; ++k) {
-            if (k0 + k < cnt) {
+            if (k0 + k < k1) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) acc[e] += x[k].get(e);
-                const bool end = (ends >> (k0 + k)) & 1;
-                if (end || k0 + k == cnt - 1) {
+                if ((cut >> (k0 + k)) & 1) {
                     if (on) {
-                        if (end && !from_before) {
-                            const uint32_t id = uint32_t(__builtin_amdgcn_readlane(int(me.y), 1 + k0 + k));
+                        if ((whole >> (k0 + k)) & 1) {
+                            const uint32_t id = uint32_t(__builtin_amdgcn_readlane(int(me.y), k0 + k));
                             float v[VEC];
 #pragma unroll
-                            for (int e = 0; e < VEC; ++e) v[e] = scale * acc[e];
-                            Pack<TT, VEC>::store(dT + int64_t(id) * E + c, v);
+                            for (int e = 0; e < VEC; ++e) v[e] = a.scale * acc[e];
+                            Pack<TT, VEC>::store(static_cast<TT *>(a.dT) + int64_t(id) * E + c, v);
                         } else {
-                            Pack<float, VEC>::store((from_before ? first : last) + chunk * E + c, acc);
+                            float *to = (begun >> (k0 + k)) & 1 ? a.last : a.first;
+                            Pack<float, VEC>::store(to + chunk * E + c, acc);
                         }
                     }
-                    from_before = false;
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
                 }
@@ -272,22 +329,36 @@ __device__ __forceinline__ void sum_chunk(const TY *dY, int64_t E, int64_t chunk
     }
 }
 
+// Sums of ids and, in workgroups of their own spread among the others so that
+// reads and writes overlap, zeros for the ids without tokens.
 template <class TY, class TT, int VEC>
-__global__ __launch_bounds__(256) void dense_chunk_kernel(const TY *dY, int64_t E, int slices, int C, float scale,
-                                                          const uint2 *order, const uint32_t *total, TT *dT,
-                                                          float *first, float *last) {
-    const uint32_t nv = *total;
-    const int64_t jobs = (int64_t(nv) + C - 1) / C * slices;
-    for (int64_t job = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6); job < jobs; job += int64_t(gridDim.x) * 4) {
-        const int64_t chunk = job / slices;
-        sum_chunk<TY, TT, VEC>(dY, E, chunk, int(job - chunk * slices), C, nv, scale, order, dT, first, last);
+__global__ __launch_bounds__(256) void dense_sum_kernel(SumArgs a) {
+    const int w = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), lane = threadIdx.x & 63;
+    const uint64_t b = blockIdx.x, all = gridDim.x;
+    const uint64_t before = b * a.sum_blocks / all;                // adding workgroups before this one
+    if ((b + 1) * a.sum_blocks / all > before) {
+        const uint32_t nv = *a.total;
+        const int64_t jobs = ((int64_t(nv) + (1 << a.lgC) - 1) >> a.lgC) * a.slices;
+        for (int64_t job = int64_t(before) * 4 + w; job < jobs; job += int64_t(a.sum_blocks) * 4) {
+            const int64_t chunk = job / a.slices;
+            sum_chunk<TY, TT, VEC>(a, chunk, int(job - chunk * a.slices), nv);
+        }
+        return;
+    }
+    constexpr int kPer = kFillIds / 4;
+    TT *dT = static_cast<TT *>(a.dT);
+    for (int64_t id0 = int64_t(b - before) * kFillIds + w * kPer; id0 < a.V;
+         id0 += int64_t(all - a.sum_blocks) * kFillIds) {
+        const bool empty = lane < kPer && id0 + lane < a.V && a.range[id0 + lane].y == 0;
+        for (uint64_t m = __ballot(empty); m; m &= m - 1) {
+            TT *row = dT + (id0 + __ffsll((unsigned long long)m) - 1) * a.E;
+            const float zero[VEC] = {};
+            for (int64_t c0 = lane * VEC; c0 < a.E; c0 += 64 * VEC) Pack<TT, VEC>::store(row + min(c0, a.E - VEC), zero);
+        }
     }
 }
 
 constexpr int kFinishWaves = 8;
-constexpr int kFinishIds = 32;         // ids of one workgroup
-constexpr int kFinishAlone = 16;       // partial rows that one wave adds by itself
-constexpr uint32_t kDone = 0xffffffffu, kNone = 0xfffffffeu;
 
 // rows [i, end) of `part` added in order, eight loads in flight
 template <int VEC>
@@ -305,47 +376,28 @@ __device__ __forceinline__ void add_rows(const float *part, int64_t i, int64_t e
     }
 }
 
-// Rows of dT that dense_chunk_kernel left: zeros for ids without tokens, and
-// the sum of the partials of ids that lie in several chunks (last[a], then
-// first[a + 1 .. a + more]).  A workgroup takes kFinishIds ids, spread over
-// the table (frequent ids are often neighbours).  blockIdx.y = 0: a wave per
-// row, all columns; every blockIdx.y: all waves on each row that has many
-// partials, its own column slices.
+// Rows of the ids with many tokens: last[a] of the chunk where the id begins,
+// then first[a + 1 .. z], a part of them by each wave of a workgroup, the
+// waves' sums added in order.  Workgroup (g, y) takes the long ids that
+// workgroup g of dense_group_kernel listed, column slices y, y + gridDim.y ..
 template <class TT, int VEC>
-__global__ __launch_bounds__(64 * kFinishWaves) void dense_finish_kernel(int64_t V, int64_t E, int lgC, float scale,
-                                                                         const uint2 *range, const float *first,
-                                                                         const float *last, TT *dT) {
-    __shared__ uint2 rows[kFinishIds];                 // (a, more), or kDone, kNone for more
-    __shared__ uint32_t many_rows;
+__global__ __launch_bounds__(64 * kFinishWaves) void dense_finish_kernel(SumArgs a, int groups) {
     __shared__ float red[kFinishWaves][64 * VEC];
-    const int t = threadIdx.x, w = t >> 6, lane = t & 63;
-    const int64_t stride = (V + kFinishIds - 1) / kFinishIds;      // groups of ids, and the distance of a group's ids
-    constexpr int64_t kCols = 64 * VEC;
-    for (int64_t group = blockIdx.x; group < stride; group += gridDim.x) {
-        __syncthreads();                               // the last group's rows are no longer read
-        if (w == 0) {
-            uint2 x = make_uint2(0, kDone);
-            const int64_t id = group + lane * stride;
-            if (lane < kFinishIds && id < V) {
-                const uint2 r = range[id];
-                const uint32_t a = r.x >> lgC, z = (r.x + r.y - 1) >> lgC;
-                x = make_uint2(a, r.y == 0 ? kNone : z == a ? kDone : z - a);
-            }
-            const uint64_t many = __ballot(x.y >= kFinishAlone && x.y < kNone);
-            if (lane < kFinishIds) rows[lane] = x;
-            if (lane == 0) many_rows = uint32_t(many);
-        }
-        __syncthreads();
-        for (uint32_t m = many_rows; m; m &= m - 1) {  // the same rows in every wave
-            const int r = __ffs(int(m)) - 1;
-            const int64_t a = rows[r].x, more = rows[r].y;
-            for (int64_t s = blockIdx.y; s * kCols < E; s += gridDim.y) {
-                const int64_t c0 = s * kCols + lane * VEC, c = c0 < E ? min(c0, E - VEC) : 0;
+    const int w = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), lane = threadIdx.x & 63;
+    const int64_t E = a.E;
+    for (int g = blockIdx.x; g < groups; g += gridDim.x) {
+        const uint32_t n = a.n_many[g];
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint32_t id = a.many[int64_t(g) * a.Q + i];
+            const uint2 r = a.range[id];
+            const int64_t at = r.x >> a.lgC, more = ((r.x + r.y - 1) >> a.lgC) - at;
+            for (int s = blockIdx.y; s < a.slices; s += gridDim.y) {
+                const int64_t c0 = int64_t(s) * 64 * VEC + lane * VEC, c = c0 < E ? min(c0, E - VEC) : 0;
                 float acc[VEC];
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-                if (w == 0) add_rows<VEC>(last, a, a + 1, E, c, acc);
-                add_rows<VEC>(first, a + 1 + more * w / kFinishWaves, a + 1 + more * (w + 1) / kFinishWaves, E, c,
+                if (w == 0) add_rows<VEC>(a.last, at, at + 1, E, c, acc);
+                add_rows<VEC>(a.first, at + 1 + more * w / kFinishWaves, at + 1 + more * (w + 1) / kFinishWaves, E, c,
                               acc);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) red[w][lane * VEC + e] = acc[e];
@@ -354,31 +406,11 @@ __global__ __launch_bounds__(64 * kFinishWaves) void dense_finish_kernel(int64_t
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
                         for (int k = 1; k < kFinishWaves; ++k) acc[e] += red[k][lane * VEC + e];
-                        acc[e] *= scale;
+                        acc[e] *= a.scale;
                     }
-                    Pack<TT, VEC>::store(dT + (group + r * stride) * E + c, acc);
+                    Pack<TT, VEC>::store(static_cast<TT *>(a.dT) + int64_t(id) * E + c, acc);
                 }
                 __syncthreads();
-            }
-        }
-        if (blockIdx.y) continue;
-        for (int r = w; r < kFinishIds; r += kFinishWaves) {
-            const uint32_t a = uint32_t(__builtin_amdgcn_readfirstlane(int(rows[r].x)));
-            const uint32_t more = uint32_t(__builtin_amdgcn_readfirstlane(int(rows[r].y)));
-            if (more == kDone || (more >= kFinishAlone && more != kNone)) continue;
-            TT *row = dT + (group + r * stride) * E;
-            for (int64_t c0 = lane * VEC; c0 < E; c0 += kCols) {
-                const int64_t c = min(c0, E - VEC);
-                float acc[VEC];
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-                if (more != kNone) {
-                    add_rows<VEC>(last, a, int64_t(a) + 1, E, c, acc);
-                    add_rows<VEC>(first, int64_t(a) + 1, int64_t(a) + 1 + more, E, c, acc);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) acc[e] *= scale;
-                }
-                Pack<TT, VEC>::store(row + c, acc);
             }
         }
     }
@@ -388,10 +420,12 @@ __global__ __launch_bounds__(64 * kFinishWaves) void dense_finish_kernel(int64_t
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 struct DenseLayout_ {
-    size_t order, range, total, first, last, bytes;
+    size_t order, range, many, n_many, total, first, last, bytes;
     int lg, Q;          // ids mod 2^lg per workgroup, ids of one workgroup
     int lgC;            // log2 of the places of one chunk
+    int few;            // tokens of an id that is never cut
     int64_t chunks;
+    int64_t groups() const { return int64_t(1) << lg; }
 };
 
 bool dense_ok(const comera_dense_embed_shape *s) {
@@ -416,9 +450,13 @@ void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L)
     L.Q = int((s->V - 1) >> L.lg) + 1;
     // longer chunks leave fewer partial rows, shorter ones more waves
     L.lgC = n < 32768 ? 4 : 5;
+    // an id that begins at a chunk's last place ends within the 64 lanes
+    L.few = std::min(64 - (1 << L.lgC), 1 << L.lgC);
     L.chunks = (n + (1 << L.lgC) - 1) >> L.lgC;
     L.order = take(8 * size_t(n));
     L.range = take(8 * size_t(s->V));
+    L.many = take(4 * size_t(L.Q) * size_t(L.groups()));
+    L.n_many = take(4 * size_t(L.groups()));
     L.total = take(4);
     L.first = take(sizeof(float) * size_t(L.chunks) * size_t(s->E));
     L.last = take(sizeof(float) * size_t(L.chunks) * size_t(s->E));
@@ -439,29 +477,18 @@ void launch_rows(const comera_dense_embed_shape *s, const int64_t *ids, int64_t 
                       static_cast<const TT *>(T), s->V, s->E, s->E, scale, static_cast<TY *>(Y), err_flag);
 }
 
-struct SumArgs {
-    const void *dY;
-    int64_t V, E;
-    float scale;
-    const uint2 *order, *range;
-    const uint32_t *total;
-    float *first, *last;
-    void *dT;
-};
-
 template <class TY, class TT, int VEC>
-void launch_sum(const SumArgs &a, const DenseLayout_ &L, hipStream_t st) {
-    constexpr int64_t kMost = 1 << 20;                 // workgroups; the kernels walk on from there
-    const int64_t slices = (a.E + 64 * VEC - 1) / (64 * VEC);
-    if (L.chunks > 0)
-        COMERA_LAUNCH((dense_chunk_kernel<TY, TT, VEC>), dim3(unsigned(std::min(kMost, (L.chunks * slices + 3) / 4))),
-                      dim3(256), 0, st, static_cast<const TY *>(a.dY), a.E, int(slices), 1 << L.lgC, a.scale, a.order,
-                      a.total, static_cast<TT *>(a.dT), a.first, a.last);
+void launch_sum(SumArgs a, const DenseLayout_ &L, hipStream_t st) {
+    a.slices = int((a.E + 64 * VEC - 1) / (64 * VEC));
+    // workgroups up to 2^20 of each kind; the kernels walk on from there
+    constexpr int64_t kMost = 1 << 20;
+    a.sum_blocks = uint32_t(std::min(kMost, (L.chunks * a.slices + 3) / 4));
+    const uint32_t fill = uint32_t(std::min(kMost, (a.V + kFillIds - 1) / kFillIds));
+    COMERA_LAUNCH((dense_sum_kernel<TY, TT, VEC>), dim3(a.sum_blocks + fill), dim3(256), 0, st, a);
+    const int64_t groups = std::min(L.groups(), a.V);
     COMERA_LAUNCH((dense_finish_kernel<TT, VEC>),
-                  dim3(unsigned(std::min<int64_t>((a.V + kFinishIds - 1) / kFinishIds, 1 << 16)),
-                       unsigned(std::min<int64_t>(slices, 16))),
-                  dim3(64 * kFinishWaves), 0, st, a.V, a.E, L.lgC, a.scale, a.range, a.first, a.last,
-                  static_cast<TT *>(a.dT));
+                  dim3(unsigned(std::min<int64_t>(groups, 1 << 16)), unsigned(std::min(a.slices, 16))),
+                  dim3(64 * kFinishWaves), 0, st, a, int(groups));
 }
 
 template <class TY, class TT>
@@ -517,14 +544,38 @@ comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, con
     if (!ws || ws_bytes < L.bytes || reinterpret_cast<uintptr_t>(ws) % 8) return COMERA_ERR_WORKSPACE;
     char *base = static_cast<char *>(ws);
     hipStream_t st = hipStream_t(stream);
-    SumArgs a{dY, s->V, s->E, scale, reinterpret_cast<uint2 *>(base + L.order),
-              reinterpret_cast<uint2 *>(base + L.range), reinterpret_cast<uint32_t *>(base + L.total),
-              reinterpret_cast<float *>(base + L.first), reinterpret_cast<float *>(base + L.last), dT};
-    const unsigned groups = unsigned(std::min<int64_t>(int64_t(1) << L.lg, s->V));
-    const GroupArgs ga{ids, n_tokens, s->V, pad_id, L.lg, L.Q, reinterpret_cast<uint2 *>(base + L.order),
-                       reinterpret_cast<uint2 *>(base + L.range), reinterpret_cast<uint32_t *>(base + L.total),
-                       err_flag};
-    COMERA_LAUNCH(dense_group_kernel, dim3(groups), dim3(kGroupThreads), size_t(4) * kGroupWaves * L.Q, st, ga);
+    GroupArgs ga{};
+    ga.ids = ids;
+    ga.n = n_tokens;
+    ga.V = s->V;
+    ga.pad = pad_id < 0 ? kNoId : uint32_t(pad_id);
+    ga.lg = L.lg;
+    ga.Q = L.Q;
+    ga.few = uint32_t(L.few);
+    ga.order = reinterpret_cast<uint2 *>(base + L.order);
+    ga.range = reinterpret_cast<uint2 *>(base + L.range);
+    ga.many = reinterpret_cast<uint32_t *>(base + L.many);
+    ga.n_many = reinterpret_cast<uint32_t *>(base + L.n_many);
+    ga.total = reinterpret_cast<uint32_t *>(base + L.total);
+    ga.err_flag = err_flag;
+    COMERA_LAUNCH(dense_group_kernel, dim3(unsigned(std::min(L.groups(), s->V))), dim3(kGroupThreads),
+                  size_t(4) * kGroupWaves * L.Q, st, ga);
+    SumArgs a{};
+    a.dY = dY;
+    a.V = s->V;
+    a.E = s->E;
+    a.lgC = L.lgC;
+    a.few = ga.few;
+    a.scale = scale;
+    a.order = ga.order;
+    a.range = ga.range;
+    a.many = ga.many;
+    a.n_many = ga.n_many;
+    a.total = ga.total;
+    a.Q = L.Q;
+    a.first = reinterpret_cast<float *>(base + L.first);
+    a.last = reinterpret_cast<float *>(base + L.last);
+    a.dT = dT;
     if (s->table == COMERA_F32 && s->act == COMERA_F32)
         launch_sum<float, float>(a, L, st);
     else if (s->table == COMERA_F32)
