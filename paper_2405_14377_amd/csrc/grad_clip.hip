@@ -28,7 +28,8 @@ namespace {
 constexpr int kChunkTensors = 128;     // tensors of one launch: their table is a kernel argument of under 4 KiB
 constexpr int kTile = 8192;            // entries that a workgroup takes at a time
 constexpr int kGradThreads = 256;
-constexpr int kGradParts = 1024;       // workgroups of the first pass over all launches (about)
+constexpr int kGradParts = 2048;       // workgroups of the first pass over all launches (about)
+constexpr int kChunkParts = 256;       // and at least so many of one launch, while it has tiles: one per CU
 constexpr int kScaleBlocks = 2048;     // workgroups of one launch of the second pass, at most
 
 struct GradChunk {
@@ -256,7 +257,7 @@ comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count,
                 c.tiles = c.tile0[c.count];
                 const int64_t n = c.tiles;
                 c.part0 = p->parts;
-                c.parts = int(std::max<int64_t>(1, std::min<int64_t>(n, int64_t(double(n) / tiles * kGradParts))));
+                c.parts = int(std::min(n, std::max<int64_t>(kChunkParts, int64_t(double(n) / tiles * kGradParts))));
                 p->parts += c.parts;
             }
             for (GradChunk &c : p->chunks) c.all_parts = p->parts;
@@ -308,9 +309,11 @@ comera_status comera_grad_clip(comera_grad_plan_t p, float scale, float max_norm
     double *part = static_cast<double *>(ws);
     for (const GradChunk &c : p->chunks)
         COMERA_LAUNCH(grad_squares_kernel, dim3(unsigned(c.parts)), dim3(kGradThreads), 0, st, c, part);
-    for (const GradChunk &c : p->chunks)
-        COMERA_LAUNCH(grad_scale_kernel, dim3(std::min<unsigned>(c.tiles, kScaleBlocks)), dim3(kGradThreads),
-                      0, st, c, part, scale, max_norm, norm, flag);
+    for (size_t i = p->chunks.size(); i-- > 0;) {      // last read, first scaled
+        const GradChunk &c = p->chunks[i];
+        COMERA_LAUNCH(grad_scale_kernel, dim3(std::min<unsigned>(c.tiles, kScaleBlocks)), dim3(kGradThreads), 0, st, c,
+                      part, scale, max_norm, norm, flag);
+    }
     return note_hip(launch_status(), "gradient clipping") ? COMERA_ERR_HIP : COMERA_OK;
 }
 
