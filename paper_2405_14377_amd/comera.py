@@ -76,11 +76,12 @@ class comera_grad_tensor(ctypes.Structure):
 
 
 _lib = None
+_torch = None          # torch, once load() has imported it
 
 
 def load(path: str = LIB_PATH) -> ctypes.CDLL:
     """Load the library once; raise if it has not been built."""
-    global _lib
+    global _lib, _torch
     if _lib is not None:
         return _lib
     if not os.path.exists(path):
@@ -91,7 +92,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     # would end up with two runtimes and the second one finds no device.
     # Loading torch first makes this library bind to torch's runtime.
     try:
-        import torch  # noqa: F401
+        import torch
+        _torch = torch
     except ImportError:
         pass
     lib = ctypes.CDLL(path)
@@ -199,7 +201,8 @@ def _ptr_array(xs: Optional[Sequence]):
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return int(torch.cuda.current_stream().cuda_stream)
+        # the handle alone: building a Stream object costs 3 us a call
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return int(stream.cuda_stream)
@@ -256,25 +259,23 @@ def block_norm_shape(width: int, stream: int = F32, act: int = F32, post: int = 
 # strided view, one that is too short or lies on another device than the
 # current one would be read wrongly or out of its bounds.
 def _dtype_of(code: int):
-    import torch
-    return torch.bfloat16 if code == BF16 else torch.float32
+    return _torch.bfloat16 if code == BF16 else _torch.float32
 
 
 def _checked(where: str, *args) -> None:
     """args: (tensor, torch dtype or None for any, entries) triples; None and raw addresses pass."""
-    import torch
-    dev = -1
+    dev = None
     for t, dtype, n in args:
-        if t is None or isinstance(t, int):
+        if t is None or t.__class__ is int:
             continue
         at = t.get_device()
-        if at < 0:
-            raise ComeraError(ERR_INVALID_ARG, f"{where}: a tensor in host memory")
-        if dev < 0:
-            dev = torch.cuda.current_device()
         if at != dev:
-            raise ComeraError(ERR_INVALID_ARG, f"{where}: a tensor on device {at}, the current device is {dev}")
-        if dtype is not None and t.dtype is not dtype:
+            if at < 0:
+                raise ComeraError(ERR_INVALID_ARG, f"{where}: a tensor in host memory")
+            dev = _torch.cuda.current_device()
+            if at != dev:
+                raise ComeraError(ERR_INVALID_ARG, f"{where}: a tensor on device {at}, the current device is {dev}")
+        if t.dtype is not dtype and dtype is not None:
             raise ComeraError(ERR_INVALID_ARG, f"{where}: {t.dtype} where {dtype} is expected")
         if not t.is_contiguous():
             raise ComeraError(ERR_INVALID_ARG, f"{where}: a tensor that is not contiguous")
@@ -462,11 +463,11 @@ def comera_dense_embed_workspace_bytes(shape: comera_dense_embed_shape, n_tokens
 
 def comera_dense_embed_forward(shape, ids, n_tokens: int, T, scale: float, Y, err_flag=None, stream=None) -> int:
     """Y[t, :] = scale * T[ids[t], :]."""
-    import torch
+    lib = load()
     where = "comera_dense_embed_forward"
-    _checked(where, (ids, torch.int64, n_tokens), (T, _dtype_of(shape.table), shape.V * shape.E),
-             (Y, _dtype_of(shape.act), n_tokens * shape.E), (err_flag, torch.int32, 1))
-    st = load().comera_dense_embed_forward(shape, _ptr(ids), n_tokens, _ptr(T), scale, _ptr(Y), _ptr(err_flag),
+    _checked(where, (ids, _torch.int64, n_tokens), (T, _dtype_of(shape.table), shape.V * shape.E),
+             (Y, _dtype_of(shape.act), n_tokens * shape.E), (err_flag, _torch.int32, 1))
+    st = lib.comera_dense_embed_forward(shape, _ptr(ids), n_tokens, _ptr(T), scale, _ptr(Y), _ptr(err_flag),
                                            _stream(stream))
     _check(st, where)
     return st
@@ -475,11 +476,11 @@ def comera_dense_embed_forward(shape, ids, n_tokens: int, T, scale: float, Y, er
 def comera_dense_embed_backward(shape, ids, n_tokens: int, dY, scale: float, pad_id: int, dT, ws, err_flag=None,
                                 stream=None) -> int:
     """dT[v, :] = scale * the sum of dY's rows of the tokens v; pad_id = -1 for none."""
-    import torch
+    lib = load()
     where = "comera_dense_embed_backward"
-    _checked(where, (ids, torch.int64, n_tokens), (dY, _dtype_of(shape.act), n_tokens * shape.E),
-             (dT, _dtype_of(shape.table), shape.V * shape.E), (ws, None, 0), (err_flag, torch.int32, 1))
-    st = load().comera_dense_embed_backward(shape, _ptr(ids), n_tokens, _ptr(dY), scale, pad_id, _ptr(dT), _ptr(ws),
+    _checked(where, (ids, _torch.int64, n_tokens), (dY, _dtype_of(shape.act), n_tokens * shape.E),
+             (dT, _dtype_of(shape.table), shape.V * shape.E), (ws, None, 0), (err_flag, _torch.int32, 1))
+    st = lib.comera_dense_embed_backward(shape, _ptr(ids), n_tokens, _ptr(dY), scale, pad_id, _ptr(dT), _ptr(ws),
                                             _nbytes(ws), _ptr(err_flag), _stream(stream))
     _check(st, where)
     return st
@@ -491,14 +492,14 @@ def comera_block_norm_workspace_bytes(shape: comera_block_norm_shape, b: int) ->
 
 def comera_block_norm_forward(shape, b: int, X, F, post_w, post_b, gate, pre_w, pre_b, Xn, H, stream=None) -> int:
     """Xn = res_scale X + branch_scale gate Npost(F), H = Npre(Xn)."""
-    import torch
+    lib = load()
     where = "comera_block_norm_forward"
-    w, f32 = shape.width, torch.float32
+    w, f32 = shape.width, _torch.float32
     st, act, e = _dtype_of(shape.stream), _dtype_of(shape.act), b * w
     _checked(where, (X, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w),
              (gate, act, e) if shape.gate == GATE_TOKEN else (gate, f32, w), (pre_w, f32, w), (pre_b, f32, w),
              (Xn, st, e), (H, act, e))
-    rc = load().comera_block_norm_forward(shape, b, _ptr(X), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
+    rc = lib.comera_block_norm_forward(shape, b, _ptr(X), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
                                           _ptr(pre_w), _ptr(pre_b), _ptr(Xn), _ptr(H), _stream(stream))
     _check(rc, where)
     return rc
@@ -507,15 +508,15 @@ def comera_block_norm_forward(shape, b: int, X, F, post_w, post_b, gate, pre_w, 
 def comera_block_norm_backward(shape, b: int, Xn, F, post_w, post_b, gate, pre_w, dXn, dH, dX, dF, dgate, dpost_w,
                                dpost_b, dpre_w, dpre_b, ws, stream=None) -> int:
     """Gradients of comera_block_norm_forward; None for an output that is not wanted."""
-    import torch
+    lib = load()
     where = "comera_block_norm_backward"
-    w, f32 = shape.width, torch.float32
+    w, f32 = shape.width, _torch.float32
     st, act, e = _dtype_of(shape.stream), _dtype_of(shape.act), b * w
     gk = (act, e) if shape.gate == GATE_TOKEN else (f32, w)
     _checked(where, (Xn, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w), (gate,) + gk, (pre_w, f32, w),
              (dXn, st, e), (dH, act, e), (dX, st, e), (dF, act, e), (dgate,) + gk, (dpost_w, f32, w),
              (dpost_b, f32, w), (dpre_w, f32, w), (dpre_b, f32, w), (ws, None, 0))
-    rc = load().comera_block_norm_backward(shape, b, _ptr(Xn), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
+    rc = lib.comera_block_norm_backward(shape, b, _ptr(Xn), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
                                            _ptr(pre_w), _ptr(dXn), _ptr(dH), _ptr(dX), _ptr(dF), _ptr(dgate),
                                            _ptr(dpost_w), _ptr(dpost_b), _ptr(dpre_w), _ptr(dpre_b), _ptr(ws),
                                            _nbytes(ws), _stream(stream))
@@ -545,18 +546,18 @@ def comera_grad_workspace_bytes(plan) -> int:
 
 def comera_grad_norm(plan, scale: float, norm, flag, ws, stream=None) -> int:
     """norm = scale * sqrt(sum of all squares); flag = 1 if it is not finite."""
-    import torch
-    _checked("comera_grad_norm", (norm, torch.float32, 1), (flag, torch.int32, 1), (ws, None, 0))
-    st = load().comera_grad_norm(plan, scale, _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws), _stream(stream))
+    lib = load()
+    _checked("comera_grad_norm", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
+    st = lib.comera_grad_norm(plan, scale, _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws), _stream(stream))
     _check(st, "comera_grad_norm")
     return st
 
 
 def comera_grad_clip(plan, scale: float, max_norm: float, norm, flag, ws, stream=None) -> int:
     """The norm, and out = scale * min(1, max_norm / norm) * g for every tensor of the plan."""
-    import torch
-    _checked("comera_grad_clip", (norm, torch.float32, 1), (flag, torch.int32, 1), (ws, None, 0))
-    st = load().comera_grad_clip(plan, scale, max_norm, _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws),
+    lib = load()
+    _checked("comera_grad_clip", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
+    st = lib.comera_grad_clip(plan, scale, max_norm, _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws),
                                  _stream(stream))
     _check(st, "comera_grad_clip")
     return st
@@ -573,15 +574,18 @@ class GradPlan:
         self.outs = [None] * len(self.grads) if outs is None else list(outs)
         if len(self.outs) != len(self.grads):
             raise ComeraError(ERR_INVALID_ARG, "GradPlan: as many outs as grads are expected")
-        arr = (comera_grad_tensor * max(1, len(self.grads)))()
-        for i, (g, o) in enumerate(zip(self.grads, self.outs)):
-            code = {"torch.float32": F32, "torch.bfloat16": BF16}.get(str(g.dtype))
+        load()
+        codes = {_torch.float32: F32, _torch.bfloat16: BF16}
+        rows = []
+        for g, o in zip(self.grads, self.outs):
+            code, n = codes.get(g.dtype), g.numel()
             if code is None:
                 raise ComeraError(ERR_INVALID_ARG, f"GradPlan: {g.dtype} gradients are not taken")
-            if o is not None and o.numel() != g.numel():
+            if o is not None and o.numel() != n:
                 raise ComeraError(ERR_INVALID_ARG, "GradPlan: an out of another size than its gradient")
             _checked("GradPlan", (g, g.dtype, 0), (o, g.dtype, 0))
-            arr[i] = comera_grad_tensor(_ptr(g), _ptr(o), g.numel(), code, 0)
+            rows.append((g.data_ptr(), None if o is None else o.data_ptr(), n, code, 0))
+        arr = (comera_grad_tensor * max(1, len(rows)))(*rows)
         self.handle = comera_grad_plan(arr, len(self.grads))
 
     @property
