@@ -67,12 +67,16 @@ struct GroupArgs {
     int64_t n, V;
     uint32_t pad;       // 2^32 - 1: none
     int lg, Q;
+    int parts;          // the tokens are walked in so many parts, by workgroups of their own
     uint32_t few;       // an id with more tokens goes to the list of long ones
     uint2 *order;       // (token, id) by id
     uint2 *range;       // (first place, tokens) of each id
-    uint32_t *many;     // [workgroup][Q] its long ids
+    uint4 *many;        // [workgroup][most_many] its long ids, (id, first place, tokens, 0)
+    int most_many;
     uint32_t *n_many;   // [workgroup] how many
     uint32_t *total;    // tokens with an id
+    uint32_t *count;    // [part][workgroup][Q] tokens of each id (more than one part)
+    uint32_t *sum;      // [part][workgroup] tokens
     int32_t *err_flag;
 };
 
@@ -96,6 +100,22 @@ __device__ __forceinline__ uint32_t good_id(const GroupArgs &a, int64_t id) {
     const uint32_t x = uint64_t(id) < uint64_t(a.V) ? uint32_t(id) : kNoId;
     return x == a.pad ? kNoId : x;
 }
+
+// set bits of m below this lane
+__device__ __forceinline__ uint32_t bits_below(uint64_t m) {
+    return __builtin_amdgcn_mbcnt_hi(uint32_t(m >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(m), 0));
+}
+
+// the tokens of a wave, of part p
+struct Segment {
+    int64_t s0, s1;
+    __device__ __forceinline__ Segment(const GroupArgs &a, int p, int w) {
+        const int64_t waves = int64_t(kGroupWaves) * a.parts;
+        const int64_t len = ((a.n + waves - 1) / waves + kGroupStep - 1) / kGroupStep * kGroupStep;
+        s0 = min(a.n, (int64_t(p) * kGroupWaves + w) * len);
+        s1 = min(a.n, s0 + len);
+    }
+};
 
 // Walks the tokens [s0, s1) of a wave; take(own, m, token, id) is called for
 // every 64 tokens of which some lanes (m) hold ids of workgroup g.  Returns
@@ -143,7 +163,7 @@ __device__ __forceinline__ void put_tokens(const GroupArgs &a, volatile uint32_t
         same &= (q >> b) & 1 ? m : ~m;
     }
     if (own) {
-        const uint32_t rank = uint32_t(__popcll(same & ((uint64_t(1) << lane) - 1)));
+        const uint32_t rank = bits_below(same);
         const uint32_t first = place[q];
         a.order[first + rank] = make_uint2(uint32_t(token_id >> 32), uint32_t(token_id));
         if (rank == 0) place[q] = first + uint32_t(__popcll(same));
@@ -159,82 +179,120 @@ __device__ __forceinline__ void put_list(const GroupArgs &a, volatile uint32_t *
     }
 }
 
-// Groups the tokens by id in one launch, in token order within an id.
-// Workgroup g owns the ids with id mod G = g (G a power of two), so that
-// frequent ids, which are often neighbours, fall to different workgroups.
-// Every workgroup reads all n ids (they stay in the L2): wave w takes a
-// contiguous part of the tokens, counts the owned ids in its own LDS
-// counters, lists the owned tokens, and counts the tokens of lower
-// workgroups, which end where this one's begin.  A prefix sum over (id, wave)
-// turns the counters into places, and the lists, in the order of the walk, go
-// to them; a wave that owns more tokens than its list holds (an id that is a
-// good part of the batch) walks its part again, list by list.  Bound by the
-// instructions of the walk, about 10 per 64 ids and wave in each of 256 CUs.
+// Tokens of each id in each part, for dense_group_kernel.
+__global__ __launch_bounds__(kGroupThreads) void dense_count_kernel(GroupArgs a) {
+    __shared__ uint32_t cnt[kGroupQ], all;
+    const int t = threadIdx.x, w = __builtin_amdgcn_readfirstlane(t >> 6);
+    const uint32_t g = blockIdx.x, p = blockIdx.y;
+    if (t < a.Q) cnt[t] = 0;
+    if (t == 0) all = 0;
+    __syncthreads();
+    const Segment seg(a, int(p), w);
+    uint32_t mine = 0;
+    walk(a, seg.s0, seg.s1, t & 63, g, [&](bool own, uint64_t m, uint32_t, uint32_t id) {
+        if (own) atomicAdd(&cnt[id >> a.lg], 1u);
+        mine += uint32_t(__popcll(m));
+    });
+    if ((t & 63) == 0) atomicAdd(&all, mine);
+    __syncthreads();
+    const int64_t at = int64_t(p) * gridDim.x + g;
+    if (t < a.Q) a.count[at * a.Q + t] = cnt[t];
+    if (t == 0) a.sum[at] = all;
+}
+
+// Groups the tokens by id, in token order within an id.  Workgroup (g, p)
+// owns the ids with id mod G = g (G a power of two), so that frequent ids,
+// which are often neighbours, fall to different workgroups, in part p of the
+// tokens.  Wave w takes a contiguous share of the part, counts the owned ids
+// in its own LDS counters and lists the owned tokens.  A prefix sum over (id,
+// wave) turns the counters into places, and the lists, in the order of the
+// walk, go to them; a wave that owns more tokens than its list holds (an id
+// that is a good part of the batch) walks its share again, list by list.
+// Where the workgroup's places begin: with one part it counts the tokens of
+// lower workgroups on the walk, which needs no other launch; with more parts
+// it adds up what dense_count_kernel counted.  Every id is read by G
+// workgroups, from the L2; bound by the instructions of the walk, about 10
+// per 64 ids and wave.
 __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a) {
     extern __shared__ uint32_t cnt[];                  // [kGroupWaves][Q]
     __shared__ uint32_t wsum[kGroupWaves], wbelow[kGroupWaves], longs;
     __shared__ uint64_t lists[kGroupWaves][kGroupList];            // token << 32 | id
     const int t = threadIdx.x, w = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, Q = a.Q;
-    const uint32_t g = blockIdx.x;
+    const uint32_t groups = gridDim.x, g = blockIdx.x, p = blockIdx.y, all = groups * a.parts;
     for (int i = t; i < kGroupWaves * Q; i += kGroupThreads) cnt[i] = 0;
     if (t == 0) longs = 0;
     __syncthreads();
-    const int64_t seg = ((a.n + kGroupWaves - 1) / kGroupWaves + kGroupStep - 1) / kGroupStep * kGroupStep;
-    const int64_t s0 = w * seg, s1 = min(a.n, s0 + seg);
+    const Segment seg(a, int(p), w);
     volatile uint64_t *list = lists[w];
     uint32_t listed = 0;
     auto append = [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
-        const uint32_t i = listed + uint32_t(__popcll(m & ((uint64_t(1) << lane) - 1)));
+        const uint32_t i = listed + bits_below(m);
         if (own && i < kGroupList) list[i] = uint64_t(token) << 32 | id;
         listed += uint32_t(__popcll(m));
     };
-    const uint32_t below = walk(a, s0, s1, lane, g, [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
+    uint32_t below = walk(a, seg.s0, seg.s1, lane, g, [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
         if (own) atomicAdd(&cnt[w * Q + int(id >> a.lg)], 1u);
         append(own, m, token, id);
     });
+    // this thread's id in all parts and in the parts before this one
+    uint32_t whole = 0, before = 0;
+    if (a.parts > 1) {
+        if (t < Q)
+            for (int x = 0; x < a.parts; ++x) {
+                const uint32_t c = a.count[(int64_t(x) * groups + g) * Q + t];
+                whole += c;
+                before += x < int(p) ? c : 0;
+            }
+        below = 0;                                     // tokens of lower workgroups, all parts
+        for (uint32_t i = t; i < all; i += kGroupThreads) below += i % groups < g ? a.sum[i] : 0;
+        for (int o = 32; o; o >>= 1) below += __shfl_xor(below, o);
+    }
     // ids out of range: every workgroup looks at its share of the tokens
     if (a.err_flag)
-        for (int64_t at = int64_t(g) * kGroupThreads + t; at < a.n; at += int64_t(gridDim.x) * kGroupThreads)
+        for (int64_t at = int64_t(p * groups + g) * kGroupThreads + t; at < a.n; at += int64_t(all) * kGroupThreads)
             if (uint64_t(a.ids[at]) >= uint64_t(a.V)) *a.err_flag = 1;
     if (lane == 0) wbelow[w] = below;
     __syncthreads();
     // thread q < Q owns one id: its total, and those of the ids before it
-    uint32_t mine = 0;
-    if (t < Q)
-        for (int x = 0; x < kGroupWaves; ++x) mine += cnt[x * Q + t];
-    uint32_t base = mine;
+    if (a.parts == 1 && t < Q)
+        for (int x = 0; x < kGroupWaves; ++x) whole += cnt[x * Q + t];
+    uint32_t base = whole;
     for (int o = 1; o < 64; o <<= 1) {
         const uint32_t y = __shfl_up(base, o);
         if (lane >= o) base += y;
     }
     if (lane == 63) wsum[w] = base;
     __syncthreads();
-    base -= mine;
+    base -= whole;
     for (int x = 0; x < kGroupWaves; ++x) {
         base += wbelow[x];
         if (x < w) base += wsum[x];
     }
     if (t < Q) {
-        const int64_t id = (int64_t(t) << a.lg) + g;
-        if (id < a.V) a.range[id] = make_uint2(base, mine);
-        if (mine > a.few) a.many[int64_t(g) * Q + atomicAdd(&longs, 1u)] = uint32_t(id);   // in any order
+        if (p == 0) {
+            const int64_t id = (int64_t(t) << a.lg) + g;
+            if (id < a.V) a.range[id] = make_uint2(base, whole);
+            if (whole > a.few)                         // in any order
+                a.many[int64_t(g) * a.most_many + atomicAdd(&longs, 1u)] = make_uint4(uint32_t(id), base, whole, 0);
+        }
+        uint32_t at = base + before;
         for (int x = 0; x < kGroupWaves; ++x) {
             const uint32_t c = cnt[x * Q + t];
-            cnt[x * Q + t] = base;
-            base += c;
+            cnt[x * Q + t] = at;
+            at += c;
         }
     }
     // all tokens with an id end behind the last id of the last workgroup
-    if (g == gridDim.x - 1 && t == kGroupThreads - 1) *a.total = base;
+    if (g == groups - 1 && p == 0 && t == kGroupThreads - 1) *a.total = base + whole;
     __syncthreads();
-    if (t == 0) a.n_many[g] = longs;
+    if (t == 0 && p == 0) a.n_many[g] = longs;
     volatile uint32_t *place = cnt + w * Q;            // this wave's places
     if (listed <= kGroupList) {
         put_list(a, place, list, listed, lane);
         return;
     }
     listed = 0;
-    walk(a, s0, s1, lane, g, [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
+    walk(a, seg.s0, seg.s1, lane, g, [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
         append(own, m, token, id);
         if (listed > kGroupList - 64) {
             put_list(a, place, list, listed, lane);
@@ -257,8 +315,9 @@ struct SumArgs {
     uint32_t few;       // tokens of an id that one wave adds alone
     float scale;
     const uint2 *order, *range;
-    const uint32_t *many, *n_many, *total;
-    int Q;
+    const uint4 *many;
+    const uint32_t *n_many, *total;
+    int most_many;
     float *first, *last;
     void *dT;
     uint32_t sum_blocks;               // of the grid's workgroups, the ones that add
@@ -358,7 +417,7 @@ __global__ __launch_bounds__(256) void dense_sum_kernel(SumArgs a) {
     }
 }
 
-constexpr int kFinishWaves = 8;
+constexpr int kFinishWaves = 16;
 
 // rows [i, end) of `part` added in order, eight loads in flight
 template <int VEC>
@@ -378,8 +437,9 @@ __device__ __forceinline__ void add_rows(const float *part, int64_t i, int64_t e
 
 // Rows of the ids with many tokens: last[a] of the chunk where the id begins,
 // then first[a + 1 .. z], a part of them by each wave of a workgroup, the
-// waves' sums added in order.  Workgroup (g, y) takes the long ids that
-// workgroup g of dense_group_kernel listed, column slices y, y + gridDim.y ..
+// waves' sums added in order.  Workgroup (g, y, z) takes every gridDim.z-th of
+// the long ids that workgroup g of dense_group_kernel listed, column slices y,
+// y + gridDim.y, ...
 template <class TT, int VEC>
 __global__ __launch_bounds__(64 * kFinishWaves) void dense_finish_kernel(SumArgs a, int groups) {
     __shared__ float red[kFinishWaves][64 * VEC];
@@ -387,10 +447,10 @@ __global__ __launch_bounds__(64 * kFinishWaves) void dense_finish_kernel(SumArgs
     const int64_t E = a.E;
     for (int g = blockIdx.x; g < groups; g += gridDim.x) {
         const uint32_t n = a.n_many[g];
-        for (uint32_t i = 0; i < n; ++i) {
-            const uint32_t id = a.many[int64_t(g) * a.Q + i];
-            const uint2 r = a.range[id];
-            const int64_t at = r.x >> a.lgC, more = ((r.x + r.y - 1) >> a.lgC) - at;
+        for (uint32_t i = blockIdx.z; i < n; i += gridDim.z) {
+            const uint4 r = a.many[int64_t(g) * a.most_many + i];
+            const uint32_t id = r.x;
+            const int64_t at = r.y >> a.lgC, more = ((r.y + r.z - 1) >> a.lgC) - at;
             for (int s = blockIdx.y; s < a.slices; s += gridDim.y) {
                 const int64_t c0 = int64_t(s) * 64 * VEC + lane * VEC, c = c0 < E ? min(c0, E - VEC) : 0;
                 float acc[VEC];
@@ -417,13 +477,19 @@ __global__ __launch_bounds__(64 * kFinishWaves) void dense_finish_kernel(SumArgs
 }
 
 // ---------------------------------------------------------------- host side
+// From here on one more launch costs less than the walk of all ids by every
+// workgroup: 16384 Zipf ids 44.1 us in one part, 45.5 in four; 32768: 56.9 and
+// 54.3; 131072: 140.7 and 96.3 (table of 32768 x 768)
+constexpr int64_t kSplitTokens = 24576;
+
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
 struct DenseLayout_ {
-    size_t order, range, many, n_many, total, first, last, bytes;
-    int lg, Q;          // ids mod 2^lg per workgroup, ids of one workgroup
+    size_t order, range, many, n_many, total, count, sum, first, last, bytes;
+    int lg, Q, parts;   // ids mod 2^lg per workgroup, ids of one workgroup, parts of the tokens
     int lgC;            // log2 of the places of one chunk
     int few;            // tokens of an id that is never cut
+    int most_many;      // most ids of one workgroup with more tokens
     int64_t chunks;
     int64_t groups() const { return int64_t(1) << lg; }
 };
@@ -444,9 +510,12 @@ void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L)
         off = align_up(off + bytes);
         return o;
     };
-    // 256 workgroups, more where one would own more ids than its LDS counts
-    L.lg = 8;
+    // 256 workgroups (more where one would own more ids than its LDS counts).
+    // A long batch is cut into parts, each id read by fewer workgroups: as
+    // few as own all ids, in as many parts as make 256 of them.
+    L.lg = n < kSplitTokens ? 8 : 5;
     while (((s->V - 1) >> L.lg) >= kGroupQ) ++L.lg;
+    L.parts = n < kSplitTokens ? 1 : std::max(1, 256 >> L.lg);
     L.Q = int((s->V - 1) >> L.lg) + 1;
     // longer chunks leave fewer partial rows, shorter ones more waves
     L.lgC = n < 32768 ? 4 : 5;
@@ -455,9 +524,14 @@ void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L)
     L.chunks = (n + (1 << L.lgC) - 1) >> L.lgC;
     L.order = take(8 * size_t(n));
     L.range = take(8 * size_t(s->V));
-    L.many = take(4 * size_t(L.Q) * size_t(L.groups()));
+    L.most_many = int(std::min<int64_t>(L.Q, n / L.few + 1));
+    L.many = take(16 * size_t(L.most_many) * size_t(L.groups()));
     L.n_many = take(4 * size_t(L.groups()));
     L.total = take(4);
+    if (L.parts > 1) {
+        L.count = take(4 * size_t(L.Q) * size_t(L.groups()) * size_t(L.parts));
+        L.sum = take(4 * size_t(L.groups()) * size_t(L.parts));
+    }
     L.first = take(sizeof(float) * size_t(L.chunks) * size_t(s->E));
     L.last = take(sizeof(float) * size_t(L.chunks) * size_t(s->E));
     L.bytes = off;
@@ -487,7 +561,8 @@ void launch_sum(SumArgs a, const DenseLayout_ &L, hipStream_t st) {
     COMERA_LAUNCH((dense_sum_kernel<TY, TT, VEC>), dim3(a.sum_blocks + fill), dim3(256), 0, st, a);
     const int64_t groups = std::min(L.groups(), a.V);
     COMERA_LAUNCH((dense_finish_kernel<TT, VEC>),
-                  dim3(unsigned(std::min<int64_t>(groups, 1 << 16)), unsigned(std::min(a.slices, 16))),
+                  dim3(unsigned(std::min<int64_t>(groups, 1 << 16)), unsigned(std::min(a.slices, 16)),
+                       unsigned(std::max<int64_t>(1, 256 / groups))),
                   dim3(64 * kFinishWaves), 0, st, a, int(groups));
 }
 
@@ -508,7 +583,7 @@ extern "C" {
 
 size_t comera_dense_embed_workspace_bytes(const comera_dense_embed_shape *s, int64_t n_tokens) {
     if (!dense_ok(s) || !dense_supported(s) || n_tokens < 0 || n_tokens >= 2147483647) return 0;
-    DenseLayout_ L;
+    DenseLayout_ L{};
     dense_layout(s, n_tokens, L);
     return L.bytes;
 }
@@ -539,7 +614,7 @@ comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, con
         return COMERA_ERR_INVALID_ARG;
     if (!dense_supported(s)) return COMERA_ERR_UNSUPPORTED;
     if (!dT || (n_tokens > 0 && (!ids || !dY))) return COMERA_ERR_INVALID_ARG;
-    DenseLayout_ L;
+    DenseLayout_ L{};
     dense_layout(s, n_tokens, L);
     if (!ws || ws_bytes < L.bytes || reinterpret_cast<uintptr_t>(ws) % 8) return COMERA_ERR_WORKSPACE;
     char *base = static_cast<char *>(ws);
@@ -554,12 +629,17 @@ comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, con
     ga.few = uint32_t(L.few);
     ga.order = reinterpret_cast<uint2 *>(base + L.order);
     ga.range = reinterpret_cast<uint2 *>(base + L.range);
-    ga.many = reinterpret_cast<uint32_t *>(base + L.many);
+    ga.many = reinterpret_cast<uint4 *>(base + L.many);
+    ga.most_many = L.most_many;
     ga.n_many = reinterpret_cast<uint32_t *>(base + L.n_many);
     ga.total = reinterpret_cast<uint32_t *>(base + L.total);
+    ga.parts = L.parts;
+    ga.count = reinterpret_cast<uint32_t *>(base + L.count);
+    ga.sum = reinterpret_cast<uint32_t *>(base + L.sum);
     ga.err_flag = err_flag;
-    COMERA_LAUNCH(dense_group_kernel, dim3(unsigned(std::min(L.groups(), s->V))), dim3(kGroupThreads),
-                  size_t(4) * kGroupWaves * L.Q, st, ga);
+    const dim3 grid(unsigned(std::min(L.groups(), s->V)), unsigned(L.parts));
+    if (L.parts > 1) COMERA_LAUNCH(dense_count_kernel, grid, dim3(kGroupThreads), 0, st, ga);
+    COMERA_LAUNCH(dense_group_kernel, grid, dim3(kGroupThreads), size_t(4) * kGroupWaves * L.Q, st, ga);
     SumArgs a{};
     a.dY = dY;
     a.V = s->V;
@@ -572,7 +652,7 @@ comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, con
     a.many = ga.many;
     a.n_many = ga.n_many;
     a.total = ga.total;
-    a.Q = L.Q;
+    a.most_many = L.most_many;
     a.first = reinterpret_cast<float *>(base + L.first);
     a.last = reinterpret_cast<float *>(base + L.last);
     a.dT = dT;
