@@ -459,13 +459,24 @@ typedef struct {
 typedef struct comera_grad_plan_s *comera_grad_plan_t;
 
 /* Lays out a list of gradient tensors (cores, rank masks, embedding tables,
- * norm weights: any number and size) for the two calls below.  Host only; the
- * plan holds the addresses, which have to stay valid while it is used, and is
- * never changed, so it may be used from several streams if each has its own
- * workspace.  No two buffers of the list may overlap (INVALID_ARG), nor be
+ * norm weights: any number and size) for the calls below.  Host only; the
+ * plan holds the addresses, which have to stay valid while it is used.  Only
+ * comera_grad_plan_set_table changes it, so it may be used from several
+ * streams if each has its own workspace.  No two buffers of the list may overlap (INVALID_ARG), nor be
  * misaligned for their dtype.  Release with comera_grad_plan_destroy. */
 comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count, comera_grad_plan_t *out);
 void comera_grad_plan_destroy(comera_grad_plan_t p);
+
+/* Long lists: the launches take their tensors 120 at a time from their
+ * arguments; with a table of all of them in device memory one launch takes
+ * them all.  comera_grad_table_bytes is the size of the table (0 where a list
+ * fits one launch and none is of use).  comera_grad_plan_set_table writes it
+ * to the caller's memory, on `stream`; later calls have to be ordered behind
+ * it, and the memory stays the plan's until the plan is destroyed or another
+ * table (or NULL: none) is set.  Not concurrently with other calls on the same
+ * plan.  A short or misaligned (8 bytes) table -> WORKSPACE. */
+size_t comera_grad_table_bytes(comera_grad_plan_t p);
+comera_status comera_grad_plan_set_table(comera_grad_plan_t p, void *table, size_t bytes, void *stream);
 
 /* Device workspace (bytes) of either call; 0 for a NULL plan. */
 size_t comera_grad_workspace_bytes(comera_grad_plan_t p);

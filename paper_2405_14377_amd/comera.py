@@ -33,7 +33,7 @@ EXPORTS = (
     "comera_dense_embed_workspace_bytes", "comera_dense_embed_forward", "comera_dense_embed_backward",
     "comera_block_norm_workspace_bytes", "comera_block_norm_forward", "comera_block_norm_backward",
     "comera_grad_plan", "comera_grad_plan_destroy", "comera_grad_workspace_bytes", "comera_grad_norm",
-    "comera_grad_clip",
+    "comera_grad_clip", "comera_grad_table_bytes", "comera_grad_plan_set_table",
 )
 FP8_QUANTIZE_WS_BYTES = 2048
 KERNEL_FWD, KERNEL_DX, KERNEL_DW = 0, 1, 2
@@ -158,6 +158,10 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.comera_grad_plan.restype = i32
     lib.comera_grad_plan_destroy.argtypes = [vp]
     lib.comera_grad_plan_destroy.restype = None
+    lib.comera_grad_table_bytes.argtypes = [vp]
+    lib.comera_grad_table_bytes.restype = sz
+    lib.comera_grad_plan_set_table.argtypes = [vp, vp, sz, vp]
+    lib.comera_grad_plan_set_table.restype = i32
     lib.comera_grad_workspace_bytes.argtypes = [vp]
     lib.comera_grad_workspace_bytes.restype = sz
     lib.comera_grad_norm.argtypes = [vp, f32, vp, vp, vp, sz, vp]
@@ -540,6 +544,19 @@ def comera_grad_plan_destroy(plan) -> None:
         load().comera_grad_plan_destroy(plan)
 
 
+def comera_grad_table_bytes(plan) -> int:
+    return int(load().comera_grad_table_bytes(plan))
+
+
+def comera_grad_plan_set_table(plan, table, stream=None) -> int:
+    """Write a long list's table to `table` (None: work without one); later calls have to be ordered behind it."""
+    lib = load()
+    _checked("comera_grad_plan_set_table", (table, None, 0))
+    st = lib.comera_grad_plan_set_table(plan, _ptr(table), _nbytes(table), _stream(stream))
+    _check(st, "comera_grad_plan_set_table")
+    return st
+
+
 def comera_grad_workspace_bytes(plan) -> int:
     return int(load().comera_grad_workspace_bytes(plan))
 
@@ -564,9 +581,10 @@ def comera_grad_clip(plan, scale: float, max_norm: float, norm, flag, ws, stream
 
 
 class GradPlan:
-    """Owns the plan of a list of gradient tensors, and keeps the tensors
-    alive.  outs: where the clipped gradients go (None, or a None entry: in
-    place)."""
+    """Owns the plan of a list of gradient tensors and a long list's table,
+    and keeps the tensors alive.  outs: where the clipped gradients go (None,
+    or a None entry: in place).  Made outside a graph capture: a table is
+    waited for, so that calls on any stream find it."""
 
     def __init__(self, grads, outs=None):
         self.handle = None
@@ -587,6 +605,12 @@ class GradPlan:
             rows.append((g.data_ptr(), None if o is None else o.data_ptr(), n, code, 0))
         arr = (comera_grad_tensor * max(1, len(rows)))(*rows)
         self.handle = comera_grad_plan(arr, len(self.grads))
+        self.table = None
+        nbytes = comera_grad_table_bytes(self.handle)
+        if nbytes:
+            self.table = _torch.empty(nbytes, dtype=_torch.uint8, device=self.grads[0].device)
+            comera_grad_plan_set_table(self.handle, self.table)
+            _torch.cuda.current_stream().synchronize()
 
     @property
     def workspace_bytes(self) -> int:

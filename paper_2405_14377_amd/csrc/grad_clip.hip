@@ -25,33 +25,73 @@
 namespace comera {
 namespace {
 
-constexpr int kChunkTensors = 128;     // tensors of one launch: their table is a kernel argument of under 4 KiB
+constexpr int kChunkTensors = 120;     // tensors of one launch whose table is a kernel argument of under 4 KiB
 constexpr int kTile = 8192;            // entries that a workgroup takes at a time
 constexpr int kGradThreads = 256;
-constexpr int kGradParts = 2048;       // workgroups of the first pass over all launches (about)
-constexpr int kChunkParts = 256;       // and at least so many of one launch, while it has tiles: one per CU
+constexpr int kGradParts = 2048;       // workgroups of the first pass over all launches, up to twice as many
 constexpr int kScaleBlocks = 2048;     // workgroups of one launch of the second pass, at most
+// From here on (bytes read and written) the clipped gradients are stored
+// around the last-level cache: their lines would leave it only during the
+// next pass, and throw out what that pass could still find there.  272 MB:
+// both passes together 110 -> 97 us.
+constexpr double kStreamBytes = 192.0 * 1048576;
+constexpr int64_t kBf16 = int64_t(1) << 62;
 
-struct GradChunk {
-    const void *g[kChunkTensors];
-    void *out[kChunkTensors];
-    int64_t n[kChunkTensors];
-    uint32_t tile0[kChunkTensors + 1]; // first tile of each tensor; behind the last one, the tiles and then 2^32 - 1
-    uint32_t tiles;
-    uint64_t is_bf16[kChunkTensors / 64];
+struct Entry {
+    const void *g;
+    void *out;
+    int64_t n;                         // entries, and kBf16
+    uint32_t tile0, tile1;             // its tiles, among those of the launch
+    __host__ __device__ __forceinline__ int64_t size() const { return n & ~kBf16; }
+    __host__ __device__ __forceinline__ bool is_bf16() const { return n & kBf16; }
+};
+
+struct Work {
     int count;
+    uint32_t tiles;
+    uint32_t per;                      // tiles of a workgroup of the first pass
     int part0, parts;                  // this launch's partials
     int all_parts;
 };
+
+// a launch's tensors as a kernel argument, and in device memory
+struct GradChunk : Work {
+    Entry e[kChunkTensors];
+    __device__ __forceinline__ Entry at(int i) const { return e[i]; }
+    __device__ __forceinline__ uint32_t tile0(int i) const { return e[i].tile0; }
+};
 static_assert(sizeof(GradChunk) <= 3968, "the table is passed as a kernel argument");
 
-// tensor that holds tile t (the last one that starts at or before it): every
-// lane compares two entries of the table, so it takes one round trip
-__device__ __forceinline__ int tensor_of(const GradChunk &c, uint32_t t) {
-    static_assert(kChunkTensors == 128, "two entries a lane");
+struct GradTable : Work {
+    const Entry *e;
+    __device__ __forceinline__ Entry at(int i) const { return e[i]; }
+    __device__ __forceinline__ uint32_t tile0(int i) const { return e[i].tile0; }
+};
+
+// Tensor that holds tile t (the last one that starts at or before it): the
+// lanes compare 64 entries of the table at a time, so 64 tensors take one
+// round trip, 4096 two.
+template <class List>
+__device__ __forceinline__ int tensor_of(const List &c, uint32_t t) {
     const int lane = threadIdx.x & 63;
-    const uint32_t x = c.tile0[lane], y = c.tile0[64 + lane];
-    return __popcll(__ballot(x <= t)) + __popcll(__ballot(y <= t)) - 1;
+    int lo = 0, len = c.count;
+    while (len > 1) {
+        const int step = (len + 63) / 64;
+        const bool le = lane * step < len && c.tile0(lo + min(lane * step, len - 1)) <= t;
+        const int k = __popcll(__ballot(le)) - 1;
+        lo += k * step;
+        len = min(step, len - k * step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// entries of one launch's table to their place in the whole list's
+__global__ __launch_bounds__(128) void grad_table_kernel(GradChunk c, Entry *table, uint32_t tile_base) {
+    if (int(threadIdx.x) >= c.count) return;
+    Entry x = c.at(threadIdx.x);
+    x.tile0 += tile_base;
+    x.tile1 += tile_base;
+    table[threadIdx.x] = x;
 }
 
 // sum over a workgroup of 256 threads in a fixed order, in every thread
@@ -113,16 +153,17 @@ __device__ __forceinline__ double tile_squares(const T *g, int64_t at, int64_t n
     return s[0] + s[1];
 }
 
-__global__ __launch_bounds__(kGradThreads) void grad_squares_kernel(GradChunk c, double *part) {
-    const uint32_t t0 = uint32_t(uint64_t(c.tiles) * blockIdx.x / c.parts);
-    const uint32_t t1 = uint32_t(uint64_t(c.tiles) * (blockIdx.x + 1) / c.parts);
+template <class List>
+__global__ __launch_bounds__(kGradThreads) void grad_squares_kernel(List c, double *part) {
+    const uint32_t t0 = blockIdx.x * c.per, t1 = min(t0 + c.per, c.tiles);
     double s = 0;
     int i = tensor_of(c, t0);
+    Entry x = c.at(i);
     for (uint32_t t = t0; t < t1; ++t) {
-        while (t >= c.tile0[i + 1]) ++i;
-        const int64_t at = int64_t(t - c.tile0[i]) * kTile;
-        s += (c.is_bf16[i >> 6] >> (i & 63)) & 1 ? tile_squares(static_cast<const bf16 *>(c.g[i]), at, c.n[i])
-                                                 : tile_squares(static_cast<const float *>(c.g[i]), at, c.n[i]);
+        while (t >= x.tile1) x = c.at(++i);
+        const int64_t at = int64_t(t - x.tile0) * kTile;
+        s += x.is_bf16() ? tile_squares(static_cast<const bf16 *>(x.g), at, x.size())
+                         : tile_squares(static_cast<const float *>(x.g), at, x.size());
     }
     s = block_sum(s);
     if (threadIdx.x == 0) part[c.part0 + blockIdx.x] = s;
@@ -147,7 +188,7 @@ __global__ __launch_bounds__(kGradThreads) void grad_norm_kernel(const double *p
     if (threadIdx.x == 0) write_norm(v, norm, flag);
 }
 
-template <class T>
+template <class T, bool STREAM>
 __device__ __forceinline__ void tile_scale(const T *g, T *out, int64_t at, int64_t n, float c) {
     constexpr int V = 16 / sizeof(T);
     for_tile<T>(
@@ -156,7 +197,7 @@ __device__ __forceinline__ void tile_scale(const T *g, T *out, int64_t at, int64
             float v[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) v[e] = c * p.get(e);
-            Pack<T, V>::store(out + i, v);
+            Pack<T, V>::template store<STREAM>(out + i, v);
         },
         [&](int64_t j) {
             Pack<T, 1> p;
@@ -166,7 +207,8 @@ __device__ __forceinline__ void tile_scale(const T *g, T *out, int64_t at, int64
         });
 }
 
-__global__ __launch_bounds__(kGradThreads) void grad_scale_kernel(GradChunk c, const double *part, float scale,
+template <class List, bool STREAM>
+__global__ __launch_bounds__(kGradThreads) void grad_scale_kernel(List c, const double *part, float scale,
                                                                   float max_norm, float *norm, int32_t *flag) {
     const double v = total_norm(part, c.all_parts, scale);
     if (c.part0 == 0 && blockIdx.x == 0 && threadIdx.x == 0) write_norm(v, norm, flag);
@@ -177,24 +219,29 @@ __global__ __launch_bounds__(kGradThreads) void grad_scale_kernel(GradChunk c, c
     const uint32_t t0 = uint32_t(uint64_t(c.tiles) * b / gridDim.x);
     const uint32_t t1 = uint32_t(uint64_t(c.tiles) * (b + 1) / gridDim.x);
     int i = tensor_of(c, t1 - 1);
+    Entry x = c.at(i);
     for (uint32_t t = t1; t-- > t0;) {
-        while (t < c.tile0[i]) --i;
-        if (f == 1.f && c.out[i] == c.g[i]) continue;
-        const int64_t at = int64_t(t - c.tile0[i]) * kTile;
-        if ((c.is_bf16[i >> 6] >> (i & 63)) & 1)
-            tile_scale(static_cast<const bf16 *>(c.g[i]), static_cast<bf16 *>(c.out[i]), at, c.n[i], f);
+        while (t < x.tile0) x = c.at(--i);
+        if (f == 1.f && x.out == x.g) continue;
+        const int64_t at = int64_t(t - x.tile0) * kTile;
+        if (x.is_bf16())
+            tile_scale<bf16, STREAM>(static_cast<const bf16 *>(x.g), static_cast<bf16 *>(x.out), at, x.size(), f);
         else
-            tile_scale(static_cast<const float *>(c.g[i]), static_cast<float *>(c.out[i]), at, c.n[i], f);
+            tile_scale<float, STREAM>(static_cast<const float *>(x.g), static_cast<float *>(x.out), at, x.size(), f);
     }
 }
 
 }  // namespace
 }  // namespace comera
 
-// the tensors' table, cut into launches (host memory only)
+// the tensors' table, cut into launches (host memory), and all of it in the
+// caller's device memory
 struct comera_grad_plan_s {
     std::vector<comera::GradChunk> chunks;
+    int64_t count = 0;
     int parts = 0;
+    bool stream = false;                   // more bytes than the last-level cache holds
+    comera::GradTable table{};             // e: null without one
 };
 
 using namespace comera;
@@ -207,6 +254,37 @@ struct Range {
     bool written;
 };
 
+comera_status grad_args(comera_grad_plan_t p, float scale, const void *ws, size_t ws_bytes) {
+    if (!p || !std::isfinite(scale) || !(scale > 0.f)) return COMERA_ERR_INVALID_ARG;
+    if (!ws || ws_bytes < comera_grad_workspace_bytes(p) || reinterpret_cast<uintptr_t>(ws) % sizeof(double))
+        return COMERA_ERR_WORKSPACE;
+    return COMERA_OK;
+}
+
+// the first pass; returns the number of partials
+int launch_squares(comera_grad_plan_t p, double *part, hipStream_t st) {
+    if (p->table.e) {
+        COMERA_LAUNCH((grad_squares_kernel<GradTable>), dim3(unsigned(p->table.parts)), dim3(kGradThreads), 0, st,
+                      p->table, part);
+        return p->table.parts;
+    }
+    for (const GradChunk &c : p->chunks)
+        COMERA_LAUNCH((grad_squares_kernel<GradChunk>), dim3(unsigned(c.parts)), dim3(kGradThreads), 0, st, c, part);
+    return p->parts;
+}
+
+template <class List>
+void launch_scale(comera_grad_plan_t p, const List &c, const double *part, float scale, float max_norm,
+                         float *norm, int32_t *flag, hipStream_t st) {
+    const dim3 grid(std::min<unsigned>(c.tiles, kScaleBlocks));
+    if (p->stream)
+        COMERA_LAUNCH((grad_scale_kernel<List, true>), grid, dim3(kGradThreads), 0, st, c, part, scale, max_norm, norm,
+                      flag);
+    else
+        COMERA_LAUNCH((grad_scale_kernel<List, false>), grid, dim3(kGradThreads), 0, st, c, part, scale, max_norm,
+                      norm, flag);
+}
+
 }  // namespace
 
 extern "C" {
@@ -217,7 +295,8 @@ comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count,
     if (count < 0 || (count > 0 && !tensors)) return COMERA_ERR_INVALID_ARG;
     try {
         std::vector<Range> ranges;
-        double tiles = 0;
+        std::vector<int64_t> order;
+        double tiles = 0, bytes_in = 0;
         for (int64_t i = 0; i < count; ++i) {
             const comera_grad_tensor &t = tensors[i];
             if (t.n < 0 || (t.dtype != COMERA_F32 && t.dtype != COMERA_BF16)) return COMERA_ERR_INVALID_ARG;
@@ -229,6 +308,8 @@ comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count,
             ranges.push_back({g, g + bytes, i, !o || o == g});
             if (o && o != g) ranges.push_back({o, o + bytes, i, true});
             tiles += double((t.n + kTile - 1) / kTile);
+            order.push_back(i);
+            bytes_in += double(bytes);
         }
         // no buffer twice: an entry would count twice in the norm, or be
         // scaled by two workgroups at once
@@ -238,29 +319,34 @@ comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count,
         if (tiles > 2147483647.0) return COMERA_ERR_UNSUPPORTED;
         comera_grad_plan_s *p = new comera_grad_plan_s;
         try {
-            for (int64_t i = 0; i < count; ++i) {
+            // the largest tensors first: they fill the card, and the launches
+            // for the many small ones behind them are short
+            std::stable_sort(order.begin(), order.end(),
+                             [&](int64_t a, int64_t b) { return tensors[a].n > tensors[b].n; });
+            for (const int64_t i : order) {
                 const comera_grad_tensor &t = tensors[i];
-                if (t.n == 0) continue;
-                if (p->chunks.empty() || p->chunks.back().count == kChunkTensors) {
-                    p->chunks.emplace_back();
-                    std::fill(p->chunks.back().tile0 + 1, p->chunks.back().tile0 + kChunkTensors + 1, 0xffffffffu);
-                }
+                if (p->chunks.empty() || p->chunks.back().count == kChunkTensors) p->chunks.emplace_back();
                 GradChunk &c = p->chunks.back();
-                const int k = c.count++;
-                c.g[k] = t.g;
-                c.out[k] = t.out ? t.out : const_cast<void *>(t.g);
-                c.n[k] = t.n;
-                c.tile0[k + 1] = c.tile0[k] + uint32_t((t.n + kTile - 1) / kTile);
-                if (t.dtype == COMERA_BF16) c.is_bf16[k >> 6] |= uint64_t(1) << (k & 63);
+                const uint32_t nt = uint32_t((t.n + kTile - 1) / kTile);
+                c.e[c.count++] = {t.g, t.out ? t.out : const_cast<void *>(t.g),
+                                  t.n | (t.dtype == COMERA_BF16 ? kBf16 : 0), c.tiles, c.tiles + nt};
+                c.tiles += nt;
             }
+            const uint32_t per = uint32_t(std::max(1.0, std::floor(tiles / kGradParts)));
             for (GradChunk &c : p->chunks) {
-                c.tiles = c.tile0[c.count];
-                const int64_t n = c.tiles;
+                c.per = per;
                 c.part0 = p->parts;
-                c.parts = int(std::min(n, std::max<int64_t>(kChunkParts, int64_t(double(n) / tiles * kGradParts))));
+                c.parts = int((c.tiles + per - 1) / per);
                 p->parts += c.parts;
             }
             for (GradChunk &c : p->chunks) c.all_parts = p->parts;
+            p->count = int64_t(order.size());
+            p->stream = 2 * bytes_in > kStreamBytes;
+            // one launch over the whole table: as many tiles a workgroup
+            p->table.count = int(p->count);
+            p->table.tiles = uint32_t(tiles);
+            p->table.per = per;
+            p->table.parts = p->table.all_parts = int((p->table.tiles + per - 1) / per);
         } catch (...) {
             delete p;
             throw;
@@ -274,15 +360,30 @@ comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count,
 
 void comera_grad_plan_destroy(comera_grad_plan_t p) { delete p; }
 
-size_t comera_grad_workspace_bytes(comera_grad_plan_t p) {
-    return p ? sizeof(double) * size_t(std::max(1, p->parts)) : 0;
+size_t comera_grad_table_bytes(comera_grad_plan_t p) {
+    return p && p->chunks.size() > 1 ? sizeof(Entry) * size_t(p->count) : 0;
 }
 
-static comera_status grad_args(comera_grad_plan_t p, float scale, const void *ws, size_t ws_bytes) {
-    if (!p || !std::isfinite(scale) || !(scale > 0.f)) return COMERA_ERR_INVALID_ARG;
-    if (!ws || ws_bytes < comera_grad_workspace_bytes(p) || reinterpret_cast<uintptr_t>(ws) % sizeof(double))
-        return COMERA_ERR_WORKSPACE;
+comera_status comera_grad_plan_set_table(comera_grad_plan_t p, void *table, size_t bytes, void *stream) {
+    if (!p) return COMERA_ERR_INVALID_ARG;
+    p->table.e = nullptr;
+    const size_t need = comera_grad_table_bytes(p);
+    if (!table || need == 0) return COMERA_OK;
+    if (bytes < need || reinterpret_cast<uintptr_t>(table) % 8) return COMERA_ERR_WORKSPACE;
+    Entry *e = static_cast<Entry *>(table);
+    uint32_t tiles = 0;
+    for (const GradChunk &c : p->chunks) {
+        COMERA_LAUNCH(grad_table_kernel, dim3(1), dim3(128), 0, hipStream_t(stream), c, e, tiles);
+        e += c.count;
+        tiles += c.tiles;
+    }
+    if (note_hip(launch_status(), "gradient table")) return COMERA_ERR_HIP;
+    p->table.e = static_cast<const Entry *>(table);
     return COMERA_OK;
+}
+
+size_t comera_grad_workspace_bytes(comera_grad_plan_t p) {
+    return p ? sizeof(double) * size_t(std::max(1, p->parts)) : 0;
 }
 
 comera_status comera_grad_norm(comera_grad_plan_t p, float scale, float *norm, int32_t *flag, void *ws,
@@ -291,9 +392,8 @@ comera_status comera_grad_norm(comera_grad_plan_t p, float scale, float *norm, i
     if (!norm && !flag) return COMERA_ERR_INVALID_ARG;
     hipStream_t st = hipStream_t(stream);
     double *part = static_cast<double *>(ws);
-    for (const GradChunk &c : p->chunks)
-        COMERA_LAUNCH(grad_squares_kernel, dim3(unsigned(c.parts)), dim3(kGradThreads), 0, st, c, part);
-    COMERA_LAUNCH(grad_norm_kernel, dim3(1), dim3(kGradThreads), 0, st, part, p->parts, scale, norm, flag);
+    const int parts = launch_squares(p, part, st);
+    COMERA_LAUNCH(grad_norm_kernel, dim3(1), dim3(kGradThreads), 0, st, part, parts, scale, norm, flag);
     return note_hip(launch_status(), "gradient norm") ? COMERA_ERR_HIP : COMERA_OK;
 }
 
@@ -307,13 +407,12 @@ comera_status comera_grad_clip(comera_grad_plan_t p, float scale, float max_norm
     }
     hipStream_t st = hipStream_t(stream);
     double *part = static_cast<double *>(ws);
-    for (const GradChunk &c : p->chunks)
-        COMERA_LAUNCH(grad_squares_kernel, dim3(unsigned(c.parts)), dim3(kGradThreads), 0, st, c, part);
-    for (size_t i = p->chunks.size(); i-- > 0;) {      // last read, first scaled
-        const GradChunk &c = p->chunks[i];
-        COMERA_LAUNCH(grad_scale_kernel, dim3(std::min<unsigned>(c.tiles, kScaleBlocks)), dim3(kGradThreads), 0, st, c,
-                      part, scale, max_norm, norm, flag);
-    }
+    launch_squares(p, part, st);
+    if (p->table.e)
+        launch_scale(p, p->table, part, scale, max_norm, norm, flag, st);
+    else
+        for (size_t i = p->chunks.size(); i-- > 0;)    // last read, first scaled
+            launch_scale(p, p->chunks[i], part, scale, max_norm, norm, flag, st);
     return note_hip(launch_status(), "gradient clipping") ? COMERA_ERR_HIP : COMERA_OK;
 }
 

@@ -18,6 +18,16 @@ struct bf16 {
 // any width and tensors that start anywhere.
 template <int BYTES, int ALIGN>
 struct Wide;
+
+// a store that leaves no line in the caches (STREAM), or an ordinary one
+template <bool STREAM, class W, class T>
+__device__ __forceinline__ void store_wide(T *p, const W &u) {
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(u, reinterpret_cast<W *>(p));
+    else
+        *reinterpret_cast<W *>(p) = u;
+}
+
 template <>
 struct Wide<16, 4> {
     typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4)));
@@ -66,6 +76,7 @@ struct Pack<float, V> {
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] = i < first ? 0.f : x[i];
     }
+    template <bool STREAM = false>
     static __device__ __forceinline__ void store(float *p, const float (&v)[V]) {
         if constexpr (V % 4 == 0) {
 #pragma unroll
@@ -73,7 +84,7 @@ struct Pack<float, V> {
                 typename Wide<16, 4>::type u;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) u[e] = __float_as_uint(v[i + e]);
-                *reinterpret_cast<typename Wide<16, 4>::type *>(p + i) = u;
+                store_wide<STREAM>(p + i, u);
             }
         } else {
 #pragma unroll
@@ -111,6 +122,7 @@ struct Pack<bf16, V> {
         for (int i = 0; i < V; i += 2)
             x[i / 2] = i + 1 < first ? 0u : i < first ? x[i / 2] & 0xffff0000u : x[i / 2];
     }
+    template <bool STREAM = false>
     static __device__ __forceinline__ void store(bf16 *p, const float (&v)[V]) {
         if constexpr (V % 8 == 0) {
 #pragma unroll
@@ -118,7 +130,7 @@ struct Pack<bf16, V> {
                 typename Wide<16, 2>::type u;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) u[e] = pack_bf16(v[i + 2 * e], v[i + 2 * e + 1]);
-                *reinterpret_cast<typename Wide<16, 2>::type *>(p + i) = u;
+                store_wide<STREAM>(p + i, u);
             }
         } else if constexpr (V % 4 == 0) {
 #pragma unroll
@@ -126,7 +138,7 @@ struct Pack<bf16, V> {
                 typename Wide<8, 2>::type u;
                 u[0] = pack_bf16(v[i], v[i + 1]);
                 u[1] = pack_bf16(v[i + 2], v[i + 3]);
-                *reinterpret_cast<typename Wide<8, 2>::type *>(p + i) = u;
+                store_wide<STREAM>(p + i, u);
             }
         } else {
             p->bits = uint16_t(pack_bf16(v[0], 0.f));

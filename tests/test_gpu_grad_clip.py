@@ -37,7 +37,7 @@ def _run(grads, dtypes, scale, max_norm, in_place=False, offset=0):
 
 
 SIZES = {"one": [1], "odd": [3, 1, 0, 17, 8193, 30], "tiles": [8192, 8191, 16385, 5], "many": [1 + 37 * i % 501 for i in range(300)],
-         "exactly a launch": [7] * 128, "one more": [7] * 129, "large": [3_000_017, 11, 700_001]}
+         "exactly a launch": [7] * 120, "one more": [7] * 121, "large": [3_000_017, 11, 700_001]}
 
 
 @pytest.mark.parametrize("sizes", list(SIZES))
@@ -112,6 +112,55 @@ def test_repeatable():
     for off in (0, 0):
         b = _run(grads, dtypes, 1.0, 0.5, offset=off)
         assert a[0] == b[0] and all(np.array_equal(x, y) for x, y in zip(a[2], b[2]))
+
+
+def test_long_lists_with_and_without_their_table():
+    """A list of several launches: the same partial sums by tensor, so norms that differ by their last digit at most."""
+    import torch
+    rng = np.random.default_rng(5)
+    n = [1 + 91 * i % 20000 for i in range(250)]
+    g = [dev(x, ("f32", "bf16")[i % 2]) for i, x in enumerate(_tensors(rng, n, [("f32", "bf16")[i % 2] for i in range(250)]))]
+    got = []
+    for table in (True, False):
+        outs = [torch.empty_like(x) for x in g]
+        plan = C.GradPlan(g, outs)
+        assert C.comera_grad_table_bytes(plan.handle) == plan.table.numel()
+        if not table:
+            C.comera_grad_plan_set_table(plan.handle, None)
+        ws = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+        norm = torch.zeros(1, device="cuda")
+        C.comera_grad_clip(plan.handle, 1.0, 0.5, norm, None, ws)
+        got.append((norm.item(), outs))
+    want = math.sqrt(sum(float(x.double().square().sum()) for x in g))
+    for norm, outs in got:
+        assert norm == pytest.approx(want, rel=2 * U)
+        for x, y in zip(g, outs):
+            half = HALF["bf16"] if x.dtype == torch.bfloat16 else 0.0
+            assert torch.allclose(y.double(), x.double() * (0.5 / want), rtol=4 * U + half * 1.01, atol=0)
+
+
+def test_tensors_beyond_the_last_level_cache():
+    """The streamed stores of a large list, at unaligned addresses too."""
+    import torch
+    torch.manual_seed(0)
+    flat = torch.empty(60_000_011, device="cuda")
+    grads = [torch.randn(30_000_001, device="cuda"), torch.randn(777, device="cuda"),
+             torch.randn(9_000_013, device="cuda").bfloat16()]
+    b16 = torch.empty(9_000_020, dtype=torch.bfloat16, device="cuda")
+    outs = [flat[1:30_000_002], flat[30_000_003:30_000_780], b16[1:9_000_014]]
+    flat.fill_(776.0)
+    b16.fill_(776.0)
+    plan = C.GradPlan(grads, outs)
+    ws = torch.empty(plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+    norm = torch.zeros(1, device="cuda")
+    C.comera_grad_clip(plan.handle, 1.0, 1.0, norm, None, ws)
+    want = math.sqrt(sum(float(x.double().square().sum()) for x in grads))
+    assert norm.item() == pytest.approx(want, rel=2 * U)
+    for x, y in zip(grads, outs):
+        half = HALF["bf16"] if x.dtype == torch.bfloat16 else 0.0
+        assert torch.allclose(y.double(), x.double() / want, rtol=4 * U + half * 1.01, atol=0)
+    assert flat[0] == 776 and flat[30_000_002] == 776 and (flat[30_000_780:] == 776).all()
+    assert b16[0] == 776 and (b16[9_000_014:] == 776).all()
 
 
 def test_more_than_2_31_entries():

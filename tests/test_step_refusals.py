@@ -173,6 +173,7 @@ def test_grad_refusals(checked):
     C.comera_grad_plan_destroy(p)
     assert C.comera_grad_workspace_bytes(None) == 0
     assert lib.comera_grad_plan(None, 0, None) == bad
+    assert lib.comera_grad_plan_set_table(None, FAKE, 1 << 20, 0) == bad and C.comera_grad_table_bytes(None) == 0
     for e in ([(None, None, 4, 0)], [(FAKE, None, -1, 0)], [(FAKE, None, 4, 2)], [(FAKE + 2, None, 4, 0)],
               [(FAKE, FAKE + 1025, 4, 1)], [(FAKE, None, 1 << 42, 0)],
               [(FAKE, None, 4, 0), (FAKE, None, 4, 0)],                       # the same tensor twice
@@ -190,7 +191,7 @@ def test_grad_refusals(checked):
 
 def test_grad_launches(checked):
     lib = C.load()
-    for sizes in ([], [1], [1] * 500, [1 << 33], [1 << 41, 5], [8192] * 128, [8193] * 129, [10 ** 7] + [30] * 1000):
+    for sizes in ([], [1], [1] * 500, [1 << 33], [1 << 41, 5], [8192] * 120, [8193] * 121, [10 ** 7] + [30] * 1000):
         entries, at = [], FAKE
         for i, n in enumerate(sizes):
             entries.append((at, None, n, i % 2))
@@ -200,6 +201,20 @@ def test_grad_launches(checked):
         w = C.comera_grad_workspace_bytes(p)
         assert lib.comera_grad_clip(p, 1.0, 1.0, FAKE, FAKE, FAKE, w, 0) == C.OK
         assert lib.comera_grad_norm(p, 1.0, FAKE, FAKE, FAKE, w, 0) == C.OK
+        # a long list's table: one launch where there were several
+        need = C.comera_grad_table_bytes(p)
+        assert (need > 0) == (len(sizes) > 120)
+        set_table = lib.comera_grad_plan_set_table
+        assert set_table(p, None, 0, 0) == C.OK and set_table(p, FAKE, need, 0) == C.OK
+        if need:
+            assert set_table(p, FAKE, need - 1, 0) == C.ERR_WORKSPACE and set_table(p, FAKE + 4, need, 0) == C.ERR_WORKSPACE
+            before = C.comera_debug_launch_log()
+            assert lib.comera_grad_clip(p, 1.0, 1.0, FAKE, FAKE, FAKE, w, 0) == C.OK
+            without = len(C.comera_debug_launch_log()) - len(before)          # a refused table is none
+            assert set_table(p, FAKE, need, 0) == C.OK
+            before = C.comera_debug_launch_log()
+            assert lib.comera_grad_clip(p, 1.0, 1.0, FAKE, FAKE, FAKE, w, 0) == C.OK
+            assert len(C.comera_debug_launch_log()) - len(before) == 2 < without
         C.comera_grad_plan_destroy(p)
 
 
