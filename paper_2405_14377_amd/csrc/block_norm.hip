@@ -41,6 +41,7 @@ struct NormArgs {
     void *Xn, *H;                      // forward
     void *dX, *dF, *dgate;             // backward (dgate of a per-token gate)
     float *part;                       // [workgroup][sums][N]
+    int want;                          // bit s: sum s is asked for
     int64_t b;
     int N, lpr, post, pre;
     float eps, a, beta;
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
     constexpr int NE = VEC * CH, NS = FULL ? 4 : 2;
     constexpr bool AHEAD = NE <= 12;       // with 16 entries a lane two tokens' rows do not fit the registers
     __shared__ __attribute__((aligned(16))) float red[2][8][4];
-    extern __shared__ float share[];       // [rows][N] when rows > 1
+    extern __shared__ float share[];       // [2][rows][N] when rows > 1
     int turn = 0;
     const int waves = p.lpr >> 6, rows = int(blockDim.x) / p.lpr;
     const int lane = int(threadIdx.x) % p.lpr;
@@ -407,20 +408,28 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
         if (p.dF && live) store_row<TA, VEC, CH>(p.dF, at, k, t);
     }
     if (!p.part) return;
-    // the workgroup's sums: its rows added in order through LDS
+    // the workgroup's sums, those that are asked for: its rows added in order
+    // through LDS, a pair of sums at a time
     float *out = p.part + int64_t(blockIdx.x) * NS * p.N;
+    if (rows == 1) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-        if (rows == 1) {
-            store_row<float, VEC, CH>(out, int64_t(s) * p.N, k, acc[s]);
-            continue;
-        }
-        store_row<float, VEC, CH>(share, int64_t(threadIdx.x / p.lpr) * p.N, k, acc[s]);
+        for (int s = 0; s < NS; ++s)
+            if ((p.want >> s) & 1) store_row<float, VEC, CH>(out, int64_t(s) * p.N, k, acc[s]);
+        return;
+    }
+    const int mine = int(threadIdx.x) / p.lpr;
+#pragma unroll
+    for (int s0 = 0; s0 < NS; s0 += 2) {
+        if (!((p.want >> s0) & 3)) continue;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) store_row<float, VEC, CH>(share, int64_t(s * rows + mine) * p.N, k, acc[s0 + s]);
         __syncthreads();
-        for (int c = threadIdx.x; c < p.N; c += int(blockDim.x)) {
-            float v = share[c];
-            for (int x = 1; x < rows; ++x) v += share[x * p.N + c];
-            out[int64_t(s) * p.N + c] = v;
+        for (int c = threadIdx.x; c < 2 * p.N; c += int(blockDim.x)) {
+            const int s = c >= p.N, col = c - s * p.N;
+            const float *x = share + s * rows * p.N + col;
+            float v = x[0];
+            for (int r = 1; r < rows; ++r) v += x[r * p.N];
+            out[int64_t(s0 + s) * p.N + col] = v;
         }
         __syncthreads();
     }
@@ -428,7 +437,7 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
 
 struct FinishArgs {
     const float *part;
-    int parts, N;
+    int parts, N, want;
     const float *gate_ch, *post_w, *post_b;
     float beta;
     float *dgate, *dpost_w, *dpost_b, *dpre_w, *dpre_b;
@@ -452,7 +461,7 @@ __global__ __launch_bounds__(kFinCols *kFinGroups) void block_norm_finish_kernel
         const int p = g + i * kFinGroups;
 #pragma unroll
         for (int s = 0; s < NS; ++s)
-            x[i][s] = p < a.parts ? a.part[(int64_t(p) * NS + s) * a.N + cc] : 0.f;
+            x[i][s] = p < a.parts && ((a.want >> s) & 1) ? a.part[(int64_t(p) * NS + s) * a.N + cc] : 0.f;
     }
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
@@ -553,7 +562,7 @@ template <class TS, class TA, bool FULL>
 void launch_bwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
     const unsigned grid = unsigned(bwd_parts(sp, p.b));
     const dim3 block(sp.threads());
-    const size_t lds = sp.rows > 1 ? sizeof(float) * sp.rows * p.N : 0;
+    const size_t lds = sp.rows > 1 ? sizeof(float) * 2 * sp.rows * p.N : 0;
     if (sp.vec == 1)
         COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 1, 1, FULL>), dim3(grid), block, lds, st, p);
     else if (sp.vec == 4)
@@ -656,6 +665,11 @@ comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64
     p.dF = dF;
     if (!channel) p.dgate = dgate;
     p.part = params ? static_cast<float *>(ws) : nullptr;
+    const bool ch_gate = channel && dgate;
+    if (full)
+        p.want = (dpost_w || ch_gate ? 1 : 0) | (dpost_b || ch_gate ? 2 : 0) | (dpre_w ? 4 : 0) | (dpre_b ? 8 : 0);
+    else
+        p.want = (dpost_w || ch_gate ? 1 : 0) | (dpre_w ? 2 : 0);
     p.b = b;
     p.N = int(s->width);
     p.post = s->post;
@@ -677,6 +691,7 @@ comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64
         f.part = p.part;
         f.parts = int(parts);
         f.N = p.N;
+        f.want = p.want;
         f.gate_ch = p.gate_ch;
         f.post_w = post_w;
         f.post_b = post_b;
