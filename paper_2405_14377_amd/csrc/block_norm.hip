@@ -47,29 +47,40 @@ struct NormArgs {
     float eps, a, beta;
 };
 
-// Sums of NV values over the lanes of a row: over a wave by exchanges; rows
-// of several waves add the waves' sums in order through one of two LDS
-// buffers in turn (a buffer is written again only after a barrier that every
-// reader of its last use has passed).  Every thread of the workgroup calls it
-// equally often when a row has several waves.
+// Sums of NV (1, 2 or 4) values over the lanes of a row, the same bits in
+// every lane.  Over a wave: the values are folded into one register, each in
+// the rows of 16 lanes of its own, then summed within the rows, which takes
+// 10 instructions for four values (four sums by themselves: about 50).  Rows
+// of several waves: the waves' sums go through one of two LDS buffers in turn
+// (a buffer is written again only after a barrier that every reader of its
+// last use has passed), eight lanes read them and exchange them.  Every
+// thread of the workgroup calls it equally often when a row has several
+// waves.
 template <int NV>
 __device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[8][4], int &turn, int waves) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = wave_sum(v[i]);
-    if (waves == 1) return;
-    static_assert(NV <= 4, "four sums at most");
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, w0 = w - w % waves;
-    if (lane == 0)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) red[turn][w][i] = v[i];
-    __syncthreads();
-    // eight lanes read the eight waves' sums at once and exchange them
-    const int x = lane & 7;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = red[turn][min(w0 + x, 7)][i];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = sum_of_8(x < waves ? v[i] : 0.f);
-    turn ^= 1;
+    static_assert(NV == 1 || NV == 2 || NV == 4, "one, two or four sums");
+    float s;
+    if constexpr (NV == 4) {
+        s = fold_16(fold_32(v[0], v[1]), fold_32(v[2], v[3]));     // rows: v0, v2, v1, v3
+    } else {
+        s = fold_32(v[0], v[NV - 1]);
+        s = fold_16(s, s);
+    }
+    s = sum_of_16(s);
+    if (waves > 1) {
+        const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, w0 = w - w % waves, x = lane & 7;
+        if ((lane & 15) == 0) red[turn][w][lane >> 4] = s;
+        __syncthreads();
+        s = red[turn][min(w0 + x, 7)][lane >> 4];
+        s = sum_of_8(x < waves ? s : 0.f);
+        turn ^= 1;
+    }
+    v[0] = lane_value(s, 0);
+    if constexpr (NV > 1) v[1] = lane_value(s, 32);
+    if constexpr (NV > 2) {
+        v[2] = lane_value(s, 16);
+        v[3] = lane_value(s, 48);
+    }
 }
 
 // columns of a lane: chunk j starts at col[j]; the last chunk of a row whose
@@ -88,6 +99,14 @@ struct Columns {
             col[j] = on[j] ? min(c, N - VEC) : 0;
             skip[j] = on[j] ? c - col[j] : VEC;
         }
+    }
+    // zeros for the entries that are not the lane's own
+    __device__ __forceinline__ void clear(float (&v)[CH * VEC]) const {
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+            if (skip[j])
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[j * VEC + e] = e < skip[j] ? 0.f : v[j * VEC + e];
     }
     // whether entry e of chunk j counts in sums
     __device__ __forceinline__ bool counts(int j, int e) const { return e >= skip[j]; }
@@ -142,27 +161,32 @@ __device__ __forceinline__ void load_param(const float *p, float otherwise, cons
 }
 
 // mean and reciprocal root of a row (mean 0 for RMS); two passes over the
-// registers for LAYER, so that no digits are lost where the mean is large
+// registers for LAYER, so that no digits are lost where the mean is large.
+// Entries that are not the lane's own are zeros in v.
 template <int VEC, int CH>
-__device__ __forceinline__ void row_stats(const float (&v)[CH * VEC], const Columns<VEC, CH> &k, int kind, int N,
+__device__ __forceinline__ void row_stats(const float (&v)[CH * VEC], const Columns<VEC, CH> &k, int kind, float inv_n,
                                           float eps, float (*red)[8][4], int &turn, int waves, float &mean,
                                           float &r) {
     mean = 0.f;
+    float q[1] = {0.f};
     if (kind == COMERA_NORM_LAYER) {
         float s[1] = {0.f};
 #pragma unroll
-        for (int i = 0; i < CH * VEC; ++i) s[0] += k.counts(i / VEC, i % VEC) ? v[i] : 0.f;
+        for (int i = 0; i < CH * VEC; ++i) s[0] += v[i];
         row_sum<1>(s, red, turn, waves);
-        mean = s[0] / float(N);
-    }
-    float q[1] = {0.f};
+        mean = s[0] * inv_n;
+        float d[CH * VEC];
 #pragma unroll
-    for (int i = 0; i < CH * VEC; ++i) {
-        const float x = v[i] - mean;
-        q[0] += k.counts(i / VEC, i % VEC) ? x * x : 0.f;
+        for (int i = 0; i < CH * VEC; ++i) d[i] = v[i] - mean;
+        k.clear(d);
+#pragma unroll
+        for (int i = 0; i < CH * VEC; ++i) q[0] += d[i] * d[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < CH * VEC; ++i) q[0] += v[i] * v[i];
     }
     row_sum<1>(q, red, turn, waves);
-    r = 1.f / sqrtf(q[0] / float(N) + eps);
+    r = rsqrtf(q[0] * inv_n + eps);
 }
 
 // the rows of one token that the forward reads, as loaded
@@ -189,6 +213,7 @@ __global__ __launch_bounds__(512) void block_norm_fwd_kernel(NormArgs p) {
     const int waves = p.lpr >> 6, rows = int(blockDim.x) / p.lpr;
     const int lane = int(threadIdx.x) % p.lpr;
     const Columns<VEC, CH> k(lane, p.lpr, p.N);
+    const float inv_n = 1.f / float(p.N);
     float pw[NE], pb[NE], w[NE], wb[NE];
     load_param<VEC, CH>(p.gate_ch, 1.f, k, pw);
     load_param<VEC, CH>(p.post_b, 0.f, k, pb);
@@ -217,9 +242,10 @@ __global__ __launch_bounds__(512) void block_norm_fwd_kernel(NormArgs p) {
             float f[NE];
 #pragma unroll
             for (int i = 0; i < NE; ++i) f[i] = in.f[i / VEC].get(i % VEC);
+            k.clear(f);
             float mean = 0.f, r = 1.f;
             if (p.post != COMERA_NORM_NONE)
-                row_stats<VEC, CH>(f, k, p.post, p.N, p.eps, red, turn, waves, mean, r);
+                row_stats<VEC, CH>(f, k, p.post, inv_n, p.eps, red, turn, waves, mean, r);
 #pragma unroll
             for (int i = 0; i < NE; ++i) {
                 float z = (f[i] - mean) * r * pw[i] + pb[i];
@@ -227,9 +253,10 @@ __global__ __launch_bounds__(512) void block_norm_fwd_kernel(NormArgs p) {
                 x[i] = p.a * x[i] + p.beta * z;
             }
         }
+        k.clear(x);
         // the pre-norm takes Xn before its rounding to the stream's type
         float mean = 0.f, r = 1.f;
-        if (p.pre != COMERA_NORM_NONE) row_stats<VEC, CH>(x, k, p.pre, p.N, p.eps, red, turn, waves, mean, r);
+        if (p.pre != COMERA_NORM_NONE) row_stats<VEC, CH>(x, k, p.pre, inv_n, p.eps, red, turn, waves, mean, r);
         if (p.Xn) store_row<TS, VEC, CH>(p.Xn, at, k, x);
         if (p.H) {
 #pragma unroll
@@ -258,14 +285,18 @@ struct BwdRows {
             if (p.gate) g[j].load(static_cast<const TA *>(p.gate) + at + k.col[j]);
         }
     }
-    __device__ __forceinline__ void clear(const NormArgs &p, const Columns<VEC, CH> &k) {
+    // zeros for the entries that are not the lane's own; a row that is not
+    // live adds nothing to any sum
+    __device__ __forceinline__ void clear(const NormArgs &p, const Columns<VEC, CH> &k, bool live) {
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            if (k.skip[j] == 0) continue;
-            t[j].clear(k.skip[j]);
-            x[j].clear(k.skip[j]);
-            h[j].clear(k.skip[j]);
-            f[j].clear(k.skip[j]);
+            const int n = live ? k.skip[j] : VEC;
+            if (n == 0) continue;
+            t[j].clear(n);
+            x[j].clear(n);
+            h[j].clear(n);
+            f[j].clear(n);
+            g[j].clear(n);
         }
     }
 };
@@ -281,7 +312,9 @@ struct BwdRows {
 template <class TS, class TA, int VEC, int CH, bool FULL>
 __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
     constexpr int NE = VEC * CH, NS = FULL ? 4 : 2;
-    constexpr bool AHEAD = NE <= 12;       // with 16 entries a lane two tokens' rows do not fit the registers
+    // two tokens' rows do not fit the registers with 16 entries a lane, nor with
+    // 12 in fp32 and every sum (4096 x 768 LAYER: 27.4 us with spills, 20.0)
+    constexpr bool AHEAD = NE <= 8 || (NE <= 12 && !(FULL && sizeof(TS) == 4 && sizeof(TA) == 4));
     __shared__ __attribute__((aligned(16))) float red[2][8][4];
     extern __shared__ float share[];       // [2][rows][N] when rows > 1
     int turn = 0;
@@ -319,7 +352,7 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
         } else {
             in.load(p, min(row, p.b - 1), k);
         }
-        in.clear(p, k);
+        in.clear(p, k, live);
         const int64_t at = row * p.N;
         float x[NE], f[NE], t[NE];
         float mean[2] = {0.f, 0.f};
@@ -333,33 +366,40 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
             mean[0] *= inv_n;
             mean[1] *= inv_n;
         }
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        if (p.dH)
 #pragma unroll
-        for (int i = 0; i < NE; ++i) {
-            const bool on = k.counts(i / VEC, i % VEC);
-            if (p.dH) {
-                x[i] = in.x[i / VEC].get(i % VEC);
-                if constexpr (FULL) x[i] = on ? x[i] - mean[0] : 0.f;
+            for (int i = 0; i < NE; ++i) x[i] = in.x[i / VEC].get(i % VEC) - (FULL ? mean[0] : 0.f);
+        if (p.F)
+#pragma unroll
+            for (int i = 0; i < NE; ++i) f[i] = in.f[i / VEC].get(i % VEC) - (FULL ? mean[1] : 0.f);
+        if constexpr (FULL) {
+            if (p.dH) k.clear(x);          // the mean is not theirs
+            if (p.F) k.clear(f);
+        }
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        if (p.dH)
+#pragma unroll
+            for (int i = 0; i < NE; ++i) {
                 const float u = in.h[i / VEC].get(i % VEC) * w[i];
                 s[0] += x[i] * x[i];
                 s[1] += u * x[i];
                 if constexpr (FULL) s[2] += u;
             }
-            if (p.F) {
-                f[i] = in.f[i / VEC].get(i % VEC);
-                if constexpr (FULL) f[i] = on ? f[i] - mean[1] : 0.f;
-                s[3] += f[i] * f[i];
-            }
-        }
+        if (p.F)
+#pragma unroll
+            for (int i = 0; i < NE; ++i) s[3] += f[i] * f[i];
         if (p.dH || (p.F && p.post != COMERA_NORM_NONE)) row_sum<4>(s, red, turn, waves);
 #pragma unroll
-        for (int i = 0; i < NE; ++i) t[i] = p.dXn ? in.t[i / VEC].get(i % VEC) : 0.f;
+        for (int i = 0; i < NE; ++i) t[i] = 0.f;
+        if (p.dXn)
+#pragma unroll
+            for (int i = 0; i < NE; ++i) t[i] = in.t[i / VEC].get(i % VEC);
         if (p.dH) {
-            const float r = 1.f / sqrtf(s[0] * inv_n + p.eps);
+            const float r = rsqrtf(s[0] * inv_n + p.eps);
             const float sy = s[1] * r * inv_n, su = pre_mean ? s[2] * inv_n : 0.f;
 #pragma unroll
             for (int i = 0; i < NE; ++i) {
-                const float h = live ? in.h[i / VEC].get(i % VEC) : 0.f, y = x[i] * r;
+                const float h = in.h[i / VEC].get(i % VEC), y = x[i] * r;
                 acc[NS / 2][i] += h * y;
                 if constexpr (FULL) acc[3][i] += h;
                 t[i] += r * (FULL ? h * w[i] - su - y * sy : h * w[i] - y * sy);
@@ -367,12 +407,14 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
         }
         if (p.dX && live) {
             float o[NE];
+            const float a = p.F ? p.a : 1.f;
 #pragma unroll
-            for (int i = 0; i < NE; ++i) o[i] = p.F ? p.a * t[i] : t[i];
+            for (int i = 0; i < NE; ++i) o[i] = a * t[i];
             store_row<TS, VEC, CH>(p.dX, at, k, o);
         }
         if (!p.F) continue;
-        const float r = p.post != COMERA_NORM_NONE ? 1.f / sqrtf(s[3] * inv_n + p.eps) : 1.f;
+        if constexpr (FULL) k.clear(t);
+        const float r = p.post != COMERA_NORM_NONE ? rsqrtf(s[3] * inv_n + p.eps) : 1.f;
 #pragma unroll
         for (int i = 0; i < NE; ++i) f[i] *= r;
         if (p.gate) {
@@ -389,15 +431,11 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
         float q[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NE; ++i) {
-            // entries that are not the lane's own: f is zero, t need not be
-            const bool on = FULL ? k.counts(i / VEC, i % VEC) : true;
-            if (live) {
-                acc[0][i] += t[i] * f[i];
-                if constexpr (FULL) acc[1][i] += t[i];
-            }
+            acc[0][i] += t[i] * f[i];
+            if constexpr (FULL) acc[1][i] += t[i];
             t[i] *= pw[i];
             q[0] += t[i] * f[i];
-            if constexpr (FULL) q[1] += on ? t[i] : 0.f;
+            if constexpr (FULL) q[1] += t[i];
         }
         if (p.post != COMERA_NORM_NONE) {
             row_sum<2>(q, red, turn, waves);

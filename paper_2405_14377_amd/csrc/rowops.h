@@ -146,30 +146,43 @@ struct Pack<bf16, V> {
     }
 };
 
-// v of the lane that the DPP control `ctrl` names, in the rows of 16 lanes
-// that `rows` names; 0 in the other rows
-template <int ctrl, int rows>
+// v of the lane that the DPP control `ctrl` names (within a row of 16 lanes)
+template <int ctrl>
 __device__ __forceinline__ float dpp(float v) {
-    return __uint_as_float(
-        uint32_t(__builtin_amdgcn_update_dpp(0, int(__float_as_uint(v)), ctrl, rows, 0xf, rows == 0xf)));
+    return __uint_as_float(uint32_t(__builtin_amdgcn_update_dpp(0, int(__float_as_uint(v)), ctrl, 0xf, 0xf, true)));
 }
 
 // sum over 8 lanes in a row, the same bits in each of them
 __device__ __forceinline__ float sum_of_8(float v) {
-    v += dpp<0xb1, 0xf>(v);      // quad_perm 1,0,3,2
-    v += dpp<0x4e, 0xf>(v);      // quad_perm 2,3,0,1
-    v += dpp<0x141, 0xf>(v);     // row_half_mirror
+    v += dpp<0xb1>(v);      // quad_perm 1,0,3,2
+    v += dpp<0x4e>(v);      // quad_perm 2,3,0,1
+    v += dpp<0x141>(v);     // row_half_mirror
     return v;
 }
 
-// Sum over the 64 lanes of a wave, the same bits in every lane: exchanges
-// within 16 lanes, then the row totals are passed up to lane 63.
-__device__ __forceinline__ float wave_sum(float v) {
+// sum over the 16 lanes of a row
+__device__ __forceinline__ float sum_of_16(float v) {
     v = sum_of_8(v);
-    v += dpp<0x140, 0xf>(v);     // row_mirror
-    v += dpp<0x142, 0xa>(v);     // row_bcast:15
-    v += dpp<0x143, 0xc>(v);     // row_bcast:31
-    return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), 63)));
+    v += dpp<0x140>(v);     // row_mirror
+    return v;
+}
+
+// Lanes 0-31: a of this lane and of the one 32 above; lanes 32-63: the same
+// of b.  One exchange and one addition for two values.
+__device__ __forceinline__ float fold_32(float a, float b) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(x[0]) + __uint_as_float(x[1]);
+}
+
+// Rows 0 and 2 of 16 lanes: a of this lane and of the one 16 above; rows 1
+// and 3: b of the one 16 below and of this lane.
+__device__ __forceinline__ float fold_16(float a, float b) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(x[0]) + __uint_as_float(x[1]);
+}
+
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), lane)));
 }
 
 }  // namespace comera
