@@ -247,10 +247,6 @@ __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a)
         for (uint32_t i = t; i < all; i += kGroupThreads) below += i % groups < g ? a.sum[i] : 0;
         for (int o = 32; o; o >>= 1) below += __shfl_xor(below, o);
     }
-    // ids out of range: every workgroup looks at its share of the tokens
-    if (a.err_flag)
-        for (int64_t at = int64_t(p * groups + g) * kGroupThreads + t; at < a.n; at += int64_t(all) * kGroupThreads)
-            if (uint64_t(a.ids[at]) >= uint64_t(a.V)) *a.err_flag = 1;
     if (lane == 0) wbelow[w] = below;
     __syncthreads();
     // thread q < Q owns one id: its total, and those of the ids before it
@@ -287,19 +283,21 @@ __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a)
     __syncthreads();
     if (t == 0 && p == 0) a.n_many[g] = longs;
     volatile uint32_t *place = cnt + w * Q;            // this wave's places
-    if (listed <= kGroupList) {
-        put_list(a, place, list, listed, lane);
-        return;
+    if (listed > kGroupList) {
+        listed = 0;
+        walk(a, seg.s0, seg.s1, lane, g, [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
+            append(own, m, token, id);
+            if (listed > kGroupList - 64) {
+                put_list(a, place, list, listed, lane);
+                listed = 0;
+            }
+        });
     }
-    listed = 0;
-    walk(a, seg.s0, seg.s1, lane, g, [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
-        append(own, m, token, id);
-        if (listed > kGroupList - 64) {
-            put_list(a, place, list, listed, lane);
-            listed = 0;
-        }
-    });
     put_list(a, place, list, listed, lane);
+    // ids out of range: every workgroup looks at its share of the tokens
+    if (a.err_flag)
+        for (int64_t at = int64_t(p * groups + g) * kGroupThreads + t; at < a.n; at += int64_t(all) * kGroupThreads)
+            if (uint64_t(a.ids[at]) >= uint64_t(a.V)) *a.err_flag = 1;
 }
 
 // ---------------------------------------------------------------- sums by id
@@ -388,17 +386,15 @@ __device__ __forceinline__ void sum_chunk(const SumArgs &a, int64_t chunk, int s
     }
 }
 
-// Sums of ids and, in workgroups of their own spread among the others so that
-// reads and writes overlap, zeros for the ids without tokens.
+// Sums of ids and, in workgroups of their own behind the adding ones, zeros
+// for the ids without tokens.
 template <class TY, class TT, int VEC>
 __global__ __launch_bounds__(256) void dense_sum_kernel(SumArgs a) {
     const int w = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), lane = threadIdx.x & 63;
-    const uint64_t b = blockIdx.x, all = gridDim.x;
-    const uint64_t before = b * a.sum_blocks / all;                // adding workgroups before this one
-    if ((b + 1) * a.sum_blocks / all > before) {
+    if (blockIdx.x < a.sum_blocks) {
         const uint32_t nv = *a.total;
         const int64_t jobs = ((int64_t(nv) + (1 << a.lgC) - 1) >> a.lgC) * a.slices;
-        for (int64_t job = int64_t(before) * 4 + w; job < jobs; job += int64_t(a.sum_blocks) * 4) {
+        for (int64_t job = int64_t(blockIdx.x) * 4 + w; job < jobs; job += int64_t(a.sum_blocks) * 4) {
             const int64_t chunk = job / a.slices;
             sum_chunk<TY, TT, VEC>(a, chunk, int(job - chunk * a.slices), nv);
         }
@@ -406,8 +402,8 @@ __global__ __launch_bounds__(256) void dense_sum_kernel(SumArgs a) {
     }
     constexpr int kPer = kFillIds / 4;
     TT *dT = static_cast<TT *>(a.dT);
-    for (int64_t id0 = int64_t(b - before) * kFillIds + w * kPer; id0 < a.V;
-         id0 += int64_t(all - a.sum_blocks) * kFillIds) {
+    for (int64_t id0 = int64_t(blockIdx.x - a.sum_blocks) * kFillIds + w * kPer; id0 < a.V;
+         id0 += int64_t(gridDim.x - a.sum_blocks) * kFillIds) {
         const bool empty = lane < kPer && id0 + lane < a.V && a.range[id0 + lane].y == 0;
         for (uint64_t m = __ballot(empty); m; m &= m - 1) {
             TT *row = dT + (id0 + __ffsll((unsigned long long)m) - 1) * a.E;
@@ -417,7 +413,96 @@ __global__ __launch_bounds__(256) void dense_sum_kernel(SumArgs a) {
     }
 }
 
-constexpr int kFinishWaves = 16;
+// ---------------------------------------------------------------- few tokens
+constexpr int kFewTokens = 1024;       // one id a thread
+constexpr int kFewQ = 64;              // most ids of one workgroup: a bit each
+constexpr int kFewLoads = 16;          // rows in flight per wave
+
+// All of a small batch's gradient in one launch.  Workgroup g owns the ids
+// with id mod G = g: it lists its tokens in order, writes zeros for its ids
+// without tokens, a wave per row, and adds the rows of the others, a wave per
+// id and column slice.  Bound by launch latency and the zeros: 300 uniform
+// ids of 2000 x 640 bf16 8.0 us (three launches: 14.5), 1000 Zipf ids of 8000
+// x 768 11.4 us (17.7), 64 ids of 20000 x 768 10.8 us (19.5).
+template <class TY, class TT, int VEC>
+__global__ __launch_bounds__(kFewTokens) void dense_few_kernel(GroupArgs a, SumArgs b) {
+    constexpr int kWaves = kFewTokens / 64;
+    __shared__ uint2 list[kFewTokens];                 // (token, id)
+    __shared__ uint32_t wcount[kWaves];
+    __shared__ unsigned long long present;
+    const int t = threadIdx.x, w = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
+    const uint32_t g = blockIdx.x, mask = (1u << a.lg) - 1;
+    if (t == 0) present = 0;
+    __syncthreads();
+    uint32_t id = kNoId;
+    if (t < a.n) {
+        id = good_id(a, a.ids[t]);
+        if (g == 0 && a.err_flag && uint64_t(a.ids[t]) >= uint64_t(a.V)) *a.err_flag = 1;
+    }
+    const bool own = id != kNoId && (id & mask) == g;
+    const uint64_t m = __ballot(own);
+    if (own) atomicOr(&present, 1ull << (id >> a.lg));
+    if (lane == 0) wcount[w] = uint32_t(__popcll(m));
+    __syncthreads();
+    uint32_t at = 0, n = 0;
+    for (int x = 0; x < kWaves; ++x) {
+        if (x == w) at = n;
+        n += wcount[x];
+    }
+    if (own) list[at + bits_below(m)] = make_uint2(uint32_t(t), id);
+    __syncthreads();
+    n = uint32_t(__builtin_amdgcn_readfirstlane(int(n)));
+    const unsigned long long all = present;
+    const int64_t E = b.E;
+    const TY *dY = static_cast<const TY *>(b.dY);
+    TT *dT = static_cast<TT *>(b.dT);
+    // ids with tokens first: their loads are on their way while zeros are written
+    int job = 0;
+    for (unsigned long long p = all; p; p &= p - 1) {
+        const uint32_t q = uint32_t(__ffsll(p)) - 1;
+        for (int s = 0; s < b.slices; ++s, ++job) {
+            if (job % kWaves != w) continue;
+            const int64_t c0 = int64_t(s) * 64 * VEC + lane * VEC, c = c0 < E ? min(c0, E - VEC) : 0;
+            float acc[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+            for (uint32_t i = 0; i < n; i += 64) {
+                const uint2 x = list[min(i + lane, n - 1)];
+                uint64_t todo = __ballot(i + lane < n && (x.y >> a.lg) == q);
+                while (todo) {
+                    Pack<TY, VEC> r[kFewLoads];
+                    int k1 = 0, bit = 0;
+#pragma unroll
+                    for (int k = 0; k < kFewLoads; ++k) {
+                        // behind the last token its row is read again
+                        if (todo) {
+                            bit = __ffsll((unsigned long long)todo) - 1;
+                            todo &= todo - 1;
+                            k1 = k + 1;
+                        }
+                        r[k].load(dY + int64_t(uint32_t(__builtin_amdgcn_readlane(int(x.x), bit))) * E + c);
+                    }
+#pragma unroll
+                    for (int k = 0; k < kFewLoads; ++k)
+                        if (k < k1)
+#pragma unroll
+                            for (int e = 0; e < VEC; ++e) acc[e] += r[k].get(e);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) acc[e] *= b.scale;
+            if (c0 < E) Pack<TT, VEC>::store(dT + ((int64_t(q) << a.lg) + g) * E + c, acc);
+        }
+    }
+    for (int q = w; q < a.Q; q += kWaves) {
+        const int64_t row = (int64_t(q) << a.lg) + g;
+        if (row >= a.V || ((all >> q) & 1)) continue;
+        const float zero[VEC] = {};
+        for (int64_t c0 = lane * VEC; c0 < E; c0 += 64 * VEC) Pack<TT, VEC>::store(dT + row * E + min(c0, E - VEC), zero);
+    }
+}
+
+constexpr int kFinishWaves = 8;
 
 // rows [i, end) of `part` added in order, eight loads in flight
 template <int VEC>
@@ -491,6 +576,7 @@ struct DenseLayout_ {
     int few;            // tokens of an id that is never cut
     int most_many;      // most ids of one workgroup with more tokens
     int64_t chunks;
+    bool few_tokens;    // all in one launch
     int64_t groups() const { return int64_t(1) << lg; }
 };
 
@@ -513,8 +599,11 @@ void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L)
     // 256 workgroups (more where one would own more ids than its LDS counts).
     // A long batch is cut into parts, each id read by fewer workgroups: as
     // few as own all ids, in as many parts as make 256 of them.
+    // A batch of one id a thread is done by one launch (with more tables rows
+    // than 2^22 its workgroups would be too many).
+    L.few_tokens = n <= kFewTokens && s->V <= int64_t(kFewQ) << 16;
     L.lg = n < kSplitTokens ? 8 : 5;
-    while (((s->V - 1) >> L.lg) >= kGroupQ) ++L.lg;
+    while (((s->V - 1) >> L.lg) >= (L.few_tokens ? kFewQ : kGroupQ)) ++L.lg;
     L.parts = n < kSplitTokens ? 1 : std::max(1, 256 >> L.lg);
     L.Q = int((s->V - 1) >> L.lg) + 1;
     // longer chunks leave fewer partial rows, shorter ones more waves
@@ -552,14 +641,21 @@ void launch_rows(const comera_dense_embed_shape *s, const int64_t *ids, int64_t 
 }
 
 template <class TY, class TT, int VEC>
-void launch_sum(SumArgs a, const DenseLayout_ &L, hipStream_t st) {
+void launch_sum(const GroupArgs &ga, SumArgs a, const DenseLayout_ &L, hipStream_t st) {
     a.slices = int((a.E + 64 * VEC - 1) / (64 * VEC));
+    const int64_t groups = std::min(L.groups(), a.V);
+    if (L.few_tokens) {
+        COMERA_LAUNCH((dense_few_kernel<TY, TT, VEC>), dim3(unsigned(groups)), dim3(kFewTokens), 0, st, ga, a);
+        return;
+    }
+    const dim3 grid(unsigned(groups), unsigned(L.parts));
+    if (L.parts > 1) COMERA_LAUNCH(dense_count_kernel, grid, dim3(kGroupThreads), 0, st, ga);
+    COMERA_LAUNCH(dense_group_kernel, grid, dim3(kGroupThreads), size_t(4) * kGroupWaves * L.Q, st, ga);
     // workgroups up to 2^20 of each kind; the kernels walk on from there
     constexpr int64_t kMost = 1 << 20;
     a.sum_blocks = uint32_t(std::min(kMost, (L.chunks * a.slices + 3) / 4));
     const uint32_t fill = uint32_t(std::min(kMost, (a.V + kFillIds - 1) / kFillIds));
     COMERA_LAUNCH((dense_sum_kernel<TY, TT, VEC>), dim3(a.sum_blocks + fill), dim3(256), 0, st, a);
-    const int64_t groups = std::min(L.groups(), a.V);
     COMERA_LAUNCH((dense_finish_kernel<TT, VEC>),
                   dim3(unsigned(std::min<int64_t>(groups, 1 << 16)), unsigned(std::min(a.slices, 16)),
                        unsigned(std::max<int64_t>(1, 256 / groups))),
@@ -567,11 +663,11 @@ void launch_sum(SumArgs a, const DenseLayout_ &L, hipStream_t st) {
 }
 
 template <class TY, class TT>
-void launch_sum(const SumArgs &a, const DenseLayout_ &L, hipStream_t st) {
+void launch_sum(const GroupArgs &ga, const SumArgs &a, const DenseLayout_ &L, hipStream_t st) {
     if (a.E >= kSumVec)
-        launch_sum<TY, TT, kSumVec>(a, L, st);
+        launch_sum<TY, TT, kSumVec>(ga, a, L, st);
     else
-        launch_sum<TY, TT, 1>(a, L, st);
+        launch_sum<TY, TT, 1>(ga, a, L, st);
 }
 
 }  // namespace
@@ -637,9 +733,6 @@ comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, con
     ga.count = reinterpret_cast<uint32_t *>(base + L.count);
     ga.sum = reinterpret_cast<uint32_t *>(base + L.sum);
     ga.err_flag = err_flag;
-    const dim3 grid(unsigned(std::min(L.groups(), s->V)), unsigned(L.parts));
-    if (L.parts > 1) COMERA_LAUNCH(dense_count_kernel, grid, dim3(kGroupThreads), 0, st, ga);
-    COMERA_LAUNCH(dense_group_kernel, grid, dim3(kGroupThreads), size_t(4) * kGroupWaves * L.Q, st, ga);
     SumArgs a{};
     a.dY = dY;
     a.V = s->V;
@@ -657,13 +750,13 @@ comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, con
     a.last = reinterpret_cast<float *>(base + L.last);
     a.dT = dT;
     if (s->table == COMERA_F32 && s->act == COMERA_F32)
-        launch_sum<float, float>(a, L, st);
+        launch_sum<float, float>(ga, a, L, st);
     else if (s->table == COMERA_F32)
-        launch_sum<bf16, float>(a, L, st);
+        launch_sum<bf16, float>(ga, a, L, st);
     else if (s->act == COMERA_F32)
-        launch_sum<float, bf16>(a, L, st);
+        launch_sum<float, bf16>(ga, a, L, st);
     else
-        launch_sum<bf16, bf16>(a, L, st);
+        launch_sum<bf16, bf16>(ga, a, L, st);
     return dense_status();
 }
 
