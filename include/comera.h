@@ -380,8 +380,8 @@ comera_status comera_dense_embed_forward(const comera_dense_embed_shape *s, cons
  * fp32 in a fixed order: bitwise reproducible.
  *   pad_id    tokens with this id give nothing; -1 for none.
  *   err_flag  as for the forward; ids outside [0, V) give nothing.
- * Errors as for the forward; pad_id outside [-1, V) -> INVALID_ARG; a missing
- * or short workspace -> WORKSPACE. */
+ * Errors as for the forward; pad_id outside [-1, V) -> INVALID_ARG; V above
+ * 2^30 -> UNSUPPORTED; a missing, short or misaligned workspace -> WORKSPACE. */
 comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, const int64_t *ids, int64_t n_tokens,
                                           const void *dY, float scale, int64_t pad_id, void *dT, void *ws,
                                           size_t ws_bytes, int32_t *err_flag, void *stream);
@@ -474,7 +474,8 @@ void comera_grad_plan_destroy(comera_grad_plan_t p);
  * to the caller's memory, on `stream`; later calls have to be ordered behind
  * it, and the memory stays the plan's until the plan is destroyed or another
  * table (or NULL: none) is set.  Not concurrently with other calls on the same
- * plan.  A short or misaligned (8 bytes) table -> WORKSPACE. */
+ * plan.  A short or misaligned (8 bytes) table -> WORKSPACE, and the plan is
+ * without one. */
 size_t comera_grad_table_bytes(comera_grad_plan_t p);
 comera_status comera_grad_plan_set_table(comera_grad_plan_t p, void *table, size_t bytes, void *stream);
 

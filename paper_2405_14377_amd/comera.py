@@ -471,7 +471,7 @@ def comera_dense_embed_forward(shape, ids, n_tokens: int, T, scale: float, Y, er
     where = "comera_dense_embed_forward"
     _checked(where, (ids, _torch.int64, n_tokens), (T, _dtype_of(shape.table), shape.V * shape.E),
              (Y, _dtype_of(shape.act), n_tokens * shape.E), (err_flag, _torch.int32, 1))
-    st = lib.comera_dense_embed_forward(shape, _ptr(ids), n_tokens, _ptr(T), scale, _ptr(Y), _ptr(err_flag),
+    st = lib.comera_dense_embed_forward(shape, _ptr(ids), int(n_tokens), _ptr(T), float(scale), _ptr(Y), _ptr(err_flag),
                                            _stream(stream))
     _check(st, where)
     return st
@@ -484,8 +484,8 @@ def comera_dense_embed_backward(shape, ids, n_tokens: int, dY, scale: float, pad
     where = "comera_dense_embed_backward"
     _checked(where, (ids, _torch.int64, n_tokens), (dY, _dtype_of(shape.act), n_tokens * shape.E),
              (dT, _dtype_of(shape.table), shape.V * shape.E), (ws, None, 0), (err_flag, _torch.int32, 1))
-    st = lib.comera_dense_embed_backward(shape, _ptr(ids), n_tokens, _ptr(dY), scale, pad_id, _ptr(dT), _ptr(ws),
-                                            _nbytes(ws), _ptr(err_flag), _stream(stream))
+    st = lib.comera_dense_embed_backward(shape, _ptr(ids), int(n_tokens), _ptr(dY), float(scale), int(pad_id),
+                                         _ptr(dT), _ptr(ws), _nbytes(ws), _ptr(err_flag), _stream(stream))
     _check(st, where)
     return st
 
@@ -503,7 +503,7 @@ def comera_block_norm_forward(shape, b: int, X, F, post_w, post_b, gate, pre_w, 
     _checked(where, (X, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w),
              (gate, act, e) if shape.gate == GATE_TOKEN else (gate, f32, w), (pre_w, f32, w), (pre_b, f32, w),
              (Xn, st, e), (H, act, e))
-    rc = lib.comera_block_norm_forward(shape, b, _ptr(X), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
+    rc = lib.comera_block_norm_forward(shape, int(b), _ptr(X), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
                                           _ptr(pre_w), _ptr(pre_b), _ptr(Xn), _ptr(H), _stream(stream))
     _check(rc, where)
     return rc
@@ -520,7 +520,7 @@ def comera_block_norm_backward(shape, b: int, Xn, F, post_w, post_b, gate, pre_w
     _checked(where, (Xn, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w), (gate,) + gk, (pre_w, f32, w),
              (dXn, st, e), (dH, act, e), (dX, st, e), (dF, act, e), (dgate,) + gk, (dpost_w, f32, w),
              (dpost_b, f32, w), (dpre_w, f32, w), (dpre_b, f32, w), (ws, None, 0))
-    rc = lib.comera_block_norm_backward(shape, b, _ptr(Xn), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
+    rc = lib.comera_block_norm_backward(shape, int(b), _ptr(Xn), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
                                            _ptr(pre_w), _ptr(dXn), _ptr(dH), _ptr(dX), _ptr(dF), _ptr(dgate),
                                            _ptr(dpost_w), _ptr(dpost_b), _ptr(dpre_w), _ptr(dpre_b), _ptr(ws),
                                            _nbytes(ws), _stream(stream))
@@ -565,7 +565,7 @@ def comera_grad_norm(plan, scale: float, norm, flag, ws, stream=None) -> int:
     """norm = scale * sqrt(sum of all squares); flag = 1 if it is not finite."""
     lib = load()
     _checked("comera_grad_norm", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
-    st = lib.comera_grad_norm(plan, scale, _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws), _stream(stream))
+    st = lib.comera_grad_norm(plan, float(scale), _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws), _stream(stream))
     _check(st, "comera_grad_norm")
     return st
 
@@ -574,7 +574,7 @@ def comera_grad_clip(plan, scale: float, max_norm: float, norm, flag, ws, stream
     """The norm, and out = scale * min(1, max_norm / norm) * g for every tensor of the plan."""
     lib = load()
     _checked("comera_grad_clip", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
-    st = lib.comera_grad_clip(plan, scale, max_norm, _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws),
+    st = lib.comera_grad_clip(plan, float(scale), float(max_norm), _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws),
                                  _stream(stream))
     _check(st, "comera_grad_clip")
     return st

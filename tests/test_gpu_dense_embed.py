@@ -51,8 +51,9 @@ def _check_backward(got, V, ids, dY, scale, pad, table):
 
 @pytest.mark.parametrize("table", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["f32", "bf16"])
-@pytest.mark.parametrize("V,E,n,offset", [(1, 1, 1, 0), (7, 3, 20, 1), (50, 8, 33, 0), (50, 9, 1, 3), (300, 100, 257, 0),
-                                          (1000, 768, 130, 0), (33, 1001, 65, 1), (20, 4097, 9, 0)])
+@pytest.mark.parametrize("V,E,n,offset", [(1, 1, 1, 0), (7, 3, 20, 1), (50, 8, 33, 0), (50, 9, 1, 3),
+                                          (300, 100, 257, 0), (1000, 768, 130, 0), (33, 1001, 65, 1),
+                                          (20, 4097, 9, 0)])
 def test_forward(V, E, n, offset, table, act):
     rng = np.random.default_rng(V + E)
     T = values(rng.standard_normal((V, E)), table)
@@ -80,8 +81,12 @@ def test_forward_ids_out_of_range():
 
 
 @pytest.mark.parametrize("kind", ["uniform", "hot", "same", "neighbours"])
-@pytest.mark.parametrize("V,E,n", [(1, 1, 1), (3, 5, 40), (255, 8, 64), (256, 12, 65), (257, 64, 1000), (1000, 33, 2049),
-                                   (4000, 96, 777), (300000, 2, 5000), (700001, 1, 300)])
+@pytest.mark.parametrize("V,E,n", [(1, 1, 1), (3, 5, 40), (255, 8, 64), (256, 12, 65), (257, 64, 1000),
+                                   (1000, 33, 2049), (4000, 96, 777), (300000, 2, 5000), (700001, 1, 300),
+                                   # the last batch of one launch, the first of three; V beyond the one launch's
+                                   (2000, 260, 1024), (2000, 260, 1025), (4194305, 1, 700), (5, 40, 3000),
+                                   # the last batch in one part, the first in several; fewer ids than workgroups
+                                   (257, 64, 24575), (257, 64, 24576), (20, 12, 30000), (70000, 4, 65537)])
 def test_backward_sizes(V, E, n, kind):
     rng = np.random.default_rng(n)
     ids, dY = _ids(rng, n, V, kind), values(rng.standard_normal((n, E)), "f32")

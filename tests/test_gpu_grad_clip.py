@@ -36,7 +36,8 @@ def _run(grads, dtypes, scale, max_norm, in_place=False, offset=0):
     return norm.item(), flag.item(), got
 
 
-SIZES = {"one": [1], "odd": [3, 1, 0, 17, 8193, 30], "tiles": [8192, 8191, 16385, 5], "many": [1 + 37 * i % 501 for i in range(300)],
+SIZES = {"one": [1], "odd": [3, 1, 0, 17, 8193, 30], "tiles": [8192, 8191, 16385, 5],
+         "many": [1 + 37 * i % 501 for i in range(300)],
          "exactly a launch": [7] * 120, "one more": [7] * 121, "large": [3_000_017, 11, 700_001]}
 
 
@@ -119,7 +120,8 @@ def test_long_lists_with_and_without_their_table():
     import torch
     rng = np.random.default_rng(5)
     n = [1 + 91 * i % 20000 for i in range(250)]
-    g = [dev(x, ("f32", "bf16")[i % 2]) for i, x in enumerate(_tensors(rng, n, [("f32", "bf16")[i % 2] for i in range(250)]))]
+    dtypes = [("f32", "bf16")[i % 2] for i in range(250)]
+    g = [dev(x, dt) for x, dt in zip(_tensors(rng, n, dtypes), dtypes)]
     got = []
     for table in (True, False):
         outs = [torch.empty_like(x) for x in g]

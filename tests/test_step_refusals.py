@@ -17,6 +17,11 @@ def checked():
     log = C.comera_debug_launch_log()
     C.comera_debug_launch_check(False)
     assert not [x for x in log if not x["ok"]]
+    # a launch counts its threads in 32 bits, and these kernels ask for no more LDS than any kernel may have
+    for x in log:
+        g, b = x["grid"], x["block"]
+        assert g[0] * b[0] * g[1] * b[1] * g[2] * b[2] < 2 ** 32, x
+        assert x["lds"] <= 64 * 1024, x
 
 
 def _addr(i):
@@ -34,7 +39,7 @@ def test_embed_refusals(checked):
         return lib.comera_dense_embed_backward(s, ids, n, dY, scale, pad, dT, ws, w, None, 0)
 
     assert fwd() == C.OK and bwd() == C.OK
-    bad = [C.dense_embed_shape(0, 8), C.dense_embed_shape(8, 0), C.dense_embed_shape(8, 8, 2), C.dense_embed_shape(8, 8, 0, -1)]
+    bad = [C.dense_embed_shape(*x) for x in ((0, 8), (8, 0), (8, 8, 2), (8, 8, 0, -1))]
     for call in (fwd, bwd):
         for b in bad:
             assert call(s=b) == C.ERR_INVALID_ARG
@@ -56,7 +61,7 @@ def test_embed_refusals(checked):
     assert bwd(n=0, ids=None, dY=None) == C.OK and bwd(n=0, ids=None, dY=None, dT=None) == C.ERR_INVALID_ARG
 
 
-@pytest.mark.parametrize("V", [1, 2, 255, 256, 257, 524288, 524289, 2 ** 31 - 2])
+@pytest.mark.parametrize("V", [1, 2, 255, 256, 257, 524288, 524289, 2 ** 30, 2 ** 30 + 1, 2 ** 31 - 2])
 @pytest.mark.parametrize("E", [1, 3, 4, 7, 8, 1001, 2 ** 20])
 def test_embed_launches(checked, V, E):
     lib = C.load()
@@ -65,8 +70,9 @@ def test_embed_launches(checked, V, E):
             s = C.dense_embed_shape(V, E, table, C.BF16)
             assert lib.comera_dense_embed_forward(s, FAKE, n, FAKE, 1.0, FAKE, None, 0) == C.OK
             ws = C.comera_dense_embed_workspace_bytes(s, n)
-            assert ws > 0
-            assert lib.comera_dense_embed_backward(s, FAKE, n, FAKE, 1.0, -1, FAKE, FAKE, ws, None, 0) == C.OK
+            assert (ws > 0) == (V <= 2 ** 30)
+            want = C.OK if V <= 2 ** 30 else C.ERR_UNSUPPORTED
+            assert lib.comera_dense_embed_backward(s, FAKE, n, FAKE, 1.0, -1, FAKE, FAKE, ws, None, 0) == want
 
 
 def _norm_calls(**k):
@@ -207,7 +213,8 @@ def test_grad_launches(checked):
         set_table = lib.comera_grad_plan_set_table
         assert set_table(p, None, 0, 0) == C.OK and set_table(p, FAKE, need, 0) == C.OK
         if need:
-            assert set_table(p, FAKE, need - 1, 0) == C.ERR_WORKSPACE and set_table(p, FAKE + 4, need, 0) == C.ERR_WORKSPACE
+            assert set_table(p, FAKE, need - 1, 0) == C.ERR_WORKSPACE
+            assert set_table(p, FAKE + 4, need, 0) == C.ERR_WORKSPACE
             before = C.comera_debug_launch_log()
             assert lib.comera_grad_clip(p, 1.0, 1.0, FAKE, FAKE, FAKE, w, 0) == C.OK
             without = len(C.comera_debug_launch_log()) - len(before)          # a refused table is none
@@ -219,7 +226,7 @@ def test_grad_launches(checked):
 
 
 def test_tensor_checks():
-    """What the binding refuses of tensors: host memory (other devices alike), another type, strides, too few entries."""
+    """What the binding refuses of tensors: host memory, another device, another type, strides, too few entries."""
     import torch
     s = C.dense_embed_shape(4, 3)
     T, ids = torch.zeros(4, 3), torch.zeros(2, dtype=torch.int64)
