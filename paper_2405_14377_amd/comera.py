@@ -266,11 +266,12 @@ def _dtype_of(code: int):
     return _torch.bfloat16 if code == BF16 else _torch.float32
 
 
-def _checked(where: str, *args) -> None:
-    """args: (tensor, torch dtype or None for any, entries) triples; None and raw addresses pass."""
-    dev = None
+def _taken(where: str, *args) -> list:
+    """Addresses of (tensor, torch dtype or None for any, entries) triples; None and raw addresses pass."""
+    dev, out = None, []
     for t, dtype, n in args:
         if t is None or t.__class__ is int:
+            out.append(t)
             continue
         at = t.get_device()
         if at != dev:
@@ -285,6 +286,8 @@ def _checked(where: str, *args) -> None:
             raise ComeraError(ERR_INVALID_ARG, f"{where}: a tensor that is not contiguous")
         if t.numel() < n:
             raise ComeraError(ERR_INVALID_ARG, f"{where}: {t.numel()} entries where {n} are expected")
+        out.append(t.data_ptr())
+    return out
 
 
 # ------------------------------------------------------------------ entry points
@@ -469,10 +472,9 @@ def comera_dense_embed_forward(shape, ids, n_tokens: int, T, scale: float, Y, er
     """Y[t, :] = scale * T[ids[t], :]."""
     lib = load()
     where = "comera_dense_embed_forward"
-    _checked(where, (ids, _torch.int64, n_tokens), (T, _dtype_of(shape.table), shape.V * shape.E),
-             (Y, _dtype_of(shape.act), n_tokens * shape.E), (err_flag, _torch.int32, 1))
-    st = lib.comera_dense_embed_forward(shape, _ptr(ids), int(n_tokens), _ptr(T), float(scale), _ptr(Y), _ptr(err_flag),
-                                           _stream(stream))
+    ids, T, Y, err_flag = _taken(where, (ids, _torch.int64, n_tokens), (T, _dtype_of(shape.table), shape.V * shape.E),
+                                 (Y, _dtype_of(shape.act), n_tokens * shape.E), (err_flag, _torch.int32, 1))
+    st = lib.comera_dense_embed_forward(shape, ids, int(n_tokens), T, float(scale), Y, err_flag, _stream(stream))
     _check(st, where)
     return st
 
@@ -482,10 +484,13 @@ def comera_dense_embed_backward(shape, ids, n_tokens: int, dY, scale: float, pad
     """dT[v, :] = scale * the sum of dY's rows of the tokens v; pad_id = -1 for none."""
     lib = load()
     where = "comera_dense_embed_backward"
-    _checked(where, (ids, _torch.int64, n_tokens), (dY, _dtype_of(shape.act), n_tokens * shape.E),
-             (dT, _dtype_of(shape.table), shape.V * shape.E), (ws, None, 0), (err_flag, _torch.int32, 1))
-    st = lib.comera_dense_embed_backward(shape, _ptr(ids), int(n_tokens), _ptr(dY), float(scale), int(pad_id),
-                                         _ptr(dT), _ptr(ws), _nbytes(ws), _ptr(err_flag), _stream(stream))
+    nbytes = _nbytes(ws)
+    ids, dY, dT, ws, err_flag = _taken(where, (ids, _torch.int64, n_tokens),
+                                       (dY, _dtype_of(shape.act), n_tokens * shape.E),
+                                       (dT, _dtype_of(shape.table), shape.V * shape.E), (ws, None, 0),
+                                       (err_flag, _torch.int32, 1))
+    st = lib.comera_dense_embed_backward(shape, ids, int(n_tokens), dY, float(scale), int(pad_id), dT, ws, nbytes,
+                                         err_flag, _stream(stream))
     _check(st, where)
     return st
 
@@ -500,11 +505,10 @@ def comera_block_norm_forward(shape, b: int, X, F, post_w, post_b, gate, pre_w, 
     where = "comera_block_norm_forward"
     w, f32 = shape.width, _torch.float32
     st, act, e = _dtype_of(shape.stream), _dtype_of(shape.act), b * w
-    _checked(where, (X, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w),
-             (gate, act, e) if shape.gate == GATE_TOKEN else (gate, f32, w), (pre_w, f32, w), (pre_b, f32, w),
-             (Xn, st, e), (H, act, e))
-    rc = lib.comera_block_norm_forward(shape, int(b), _ptr(X), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
-                                          _ptr(pre_w), _ptr(pre_b), _ptr(Xn), _ptr(H), _stream(stream))
+    p = _taken(where, (X, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w),
+               (gate, act, e) if shape.gate == GATE_TOKEN else (gate, f32, w), (pre_w, f32, w), (pre_b, f32, w),
+               (Xn, st, e), (H, act, e))
+    rc = lib.comera_block_norm_forward(shape, int(b), *p, _stream(stream))
     _check(rc, where)
     return rc
 
@@ -517,13 +521,10 @@ def comera_block_norm_backward(shape, b: int, Xn, F, post_w, post_b, gate, pre_w
     w, f32 = shape.width, _torch.float32
     st, act, e = _dtype_of(shape.stream), _dtype_of(shape.act), b * w
     gk = (act, e) if shape.gate == GATE_TOKEN else (f32, w)
-    _checked(where, (Xn, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w), (gate,) + gk, (pre_w, f32, w),
-             (dXn, st, e), (dH, act, e), (dX, st, e), (dF, act, e), (dgate,) + gk, (dpost_w, f32, w),
-             (dpost_b, f32, w), (dpre_w, f32, w), (dpre_b, f32, w), (ws, None, 0))
-    rc = lib.comera_block_norm_backward(shape, int(b), _ptr(Xn), _ptr(F), _ptr(post_w), _ptr(post_b), _ptr(gate),
-                                           _ptr(pre_w), _ptr(dXn), _ptr(dH), _ptr(dX), _ptr(dF), _ptr(dgate),
-                                           _ptr(dpost_w), _ptr(dpost_b), _ptr(dpre_w), _ptr(dpre_b), _ptr(ws),
-                                           _nbytes(ws), _stream(stream))
+    p = _taken(where, (Xn, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w), (gate,) + gk, (pre_w, f32, w),
+               (dXn, st, e), (dH, act, e), (dX, st, e), (dF, act, e), (dgate,) + gk, (dpost_w, f32, w),
+               (dpost_b, f32, w), (dpre_w, f32, w), (dpre_b, f32, w), (ws, None, 0))
+    rc = lib.comera_block_norm_backward(shape, int(b), *p, _nbytes(ws), _stream(stream))
     _check(rc, where)
     return rc
 
@@ -551,8 +552,8 @@ def comera_grad_table_bytes(plan) -> int:
 def comera_grad_plan_set_table(plan, table, stream=None) -> int:
     """Write a long list's table to `table` (None: work without one); later calls have to be ordered behind it."""
     lib = load()
-    _checked("comera_grad_plan_set_table", (table, None, 0))
-    st = lib.comera_grad_plan_set_table(plan, _ptr(table), _nbytes(table), _stream(stream))
+    p = _taken("comera_grad_plan_set_table", (table, None, 0))
+    st = lib.comera_grad_plan_set_table(plan, *p, _nbytes(table), _stream(stream))
     _check(st, "comera_grad_plan_set_table")
     return st
 
@@ -564,8 +565,8 @@ def comera_grad_workspace_bytes(plan) -> int:
 def comera_grad_norm(plan, scale: float, norm, flag, ws, stream=None) -> int:
     """norm = scale * sqrt(sum of all squares); flag = 1 if it is not finite."""
     lib = load()
-    _checked("comera_grad_norm", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
-    st = lib.comera_grad_norm(plan, float(scale), _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws), _stream(stream))
+    p = _taken("comera_grad_norm", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
+    st = lib.comera_grad_norm(plan, float(scale), *p, _nbytes(ws), _stream(stream))
     _check(st, "comera_grad_norm")
     return st
 
@@ -573,9 +574,8 @@ def comera_grad_norm(plan, scale: float, norm, flag, ws, stream=None) -> int:
 def comera_grad_clip(plan, scale: float, max_norm: float, norm, flag, ws, stream=None) -> int:
     """The norm, and out = scale * min(1, max_norm / norm) * g for every tensor of the plan."""
     lib = load()
-    _checked("comera_grad_clip", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
-    st = lib.comera_grad_clip(plan, float(scale), float(max_norm), _ptr(norm), _ptr(flag), _ptr(ws), _nbytes(ws),
-                                 _stream(stream))
+    p = _taken("comera_grad_clip", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
+    st = lib.comera_grad_clip(plan, float(scale), float(max_norm), *p, _nbytes(ws), _stream(stream))
     _check(st, "comera_grad_clip")
     return st
 
@@ -601,8 +601,8 @@ class GradPlan:
                 raise ComeraError(ERR_INVALID_ARG, f"GradPlan: {g.dtype} gradients are not taken")
             if o is not None and o.numel() != n:
                 raise ComeraError(ERR_INVALID_ARG, "GradPlan: an out of another size than its gradient")
-            _checked("GradPlan", (g, g.dtype, 0), (o, g.dtype, 0))
-            rows.append((g.data_ptr(), None if o is None else o.data_ptr(), n, code, 0))
+            at = _taken("GradPlan", (g, g.dtype, 0), (o, g.dtype, 0))
+            rows.append((at[0], at[1], n, code, 0))
         arr = (comera_grad_tensor * max(1, len(rows)))(*rows)
         self.handle = comera_grad_plan(arr, len(self.grads))
         self.table = None
