@@ -485,45 +485,51 @@ constexpr int kFinCols = 32, kFinGroups = 32;
 
 // Sums of the workgroups' partials and the parameters' gradients from them:
 // 32 columns x 32 groups of partials per workgroup (a thread has all its
-// loads in flight at once), the groups added in order.
-template <int NS>
+// loads in flight at once), the groups added in order.  blockIdx.y = 0: the
+// NP sums of the post-norm and the gate; 1: those of the pre-norm.
+template <int NP>
 __global__ __launch_bounds__(kFinCols *kFinGroups) void block_norm_finish_kernel(FinishArgs a) {
-    constexpr int kPer = kMaxParts / kFinGroups;
-    __shared__ float red[NS][kFinGroups][kFinCols];
+    constexpr int kPer = kMaxParts / kFinGroups, NS = 2 * NP;
+    __shared__ float red[NP][kFinGroups][kFinCols];
+    const int s0 = blockIdx.y * NP;
+    if (!((a.want >> s0) & (NP == 2 ? 3 : 1))) return;
     const int l = threadIdx.x % kFinCols, g = threadIdx.x / kFinCols;
     const int c = blockIdx.x * kFinCols + l;
-    float v[NS], x[kPer][NS];
+    float x[kPer][NP];
     const int cc = min(c, a.N - 1);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int p = g + i * kFinGroups;
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
-            x[i][s] = p < a.parts && ((a.want >> s) & 1) ? a.part[(int64_t(p) * NS + s) * a.N + cc] : 0.f;
+        for (int s = 0; s < NP; ++s)
+            x[i][s] = p < a.parts ? a.part[(int64_t(p) * NS + s0 + s) * a.N + cc] : 0.f;
     }
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-        v[s] = 0.f;
+    for (int s = 0; s < NP; ++s) {
+        float v = 0.f;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) v[s] += x[i][s];
-        red[s][g][l] = v[s];
+        for (int i = 0; i < kPer; ++i) v += x[i][s];
+        red[s][g][l] = v;
     }
     __syncthreads();
-    if (g < NS) {                          // group s adds sum s ...
+    if (g < NP) {                          // group s adds sum s ...
         float sum = 0.f;
         for (int i = 0; i < kFinGroups; ++i) sum += red[g][i][l];
         red[g][0][l] = sum;                // read by this thread alone so far
     }
     __syncthreads();
     if (g != 0 || c >= a.N) return;        // ... and group 0 forms the gradients
-    const float yT = red[0][0][l], T = NS == 4 ? red[1][0][l] : 0.f, yH = red[NS / 2][0][l];
-    const float gate = a.gate_ch ? a.gate_ch[c] : 1.f;
-    if (a.dpost_w) a.dpost_w[c] = a.beta * gate * yT;
-    if (a.dpost_b) a.dpost_b[c] = a.beta * gate * T;
-    if (a.dgate)
-        a.dgate[c] = a.beta * (yT * (a.post_w ? a.post_w[c] : 1.f) + (a.post_b ? a.post_b[c] * T : 0.f));
-    if (a.dpre_w) a.dpre_w[c] = yH;
-    if (NS == 4 && a.dpre_b) a.dpre_b[c] = red[NS - 1][0][l];
+    const float first = red[0][0][l], second = NP == 2 ? red[NP - 1][0][l] : 0.f;
+    if (blockIdx.y == 0) {                 // of y_F times T, of T
+        const float gate = a.gate_ch ? a.gate_ch[c] : 1.f;
+        if (a.dpost_w) a.dpost_w[c] = a.beta * gate * first;
+        if (a.dpost_b) a.dpost_b[c] = a.beta * gate * second;
+        if (a.dgate)
+            a.dgate[c] = a.beta * (first * (a.post_w ? a.post_w[c] : 1.f) + (a.post_b ? a.post_b[c] * second : 0.f));
+    } else {                               // of dH times y_X, of dH
+        if (a.dpre_w) a.dpre_w[c] = first;
+        if (a.dpre_b) a.dpre_b[c] = second;
+    }
 }
 
 // ---------------------------------------------------------------- host side
@@ -739,11 +745,11 @@ comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64
         f.dpost_b = dpost_b;
         f.dpre_w = dpre_w;
         f.dpre_b = dpre_b;
-        const dim3 grid(unsigned((p.N + kFinCols - 1) / kFinCols)), block(kFinCols * kFinGroups);
+        const dim3 grid(unsigned((p.N + kFinCols - 1) / kFinCols), 2), block(kFinCols * kFinGroups);
         if (full)
-            COMERA_LAUNCH((block_norm_finish_kernel<4>), grid, block, 0, st, f);
-        else
             COMERA_LAUNCH((block_norm_finish_kernel<2>), grid, block, 0, st, f);
+        else
+            COMERA_LAUNCH((block_norm_finish_kernel<1>), grid, block, 0, st, f);
     }
     return note_hip(launch_status(), "block norm") ? COMERA_ERR_HIP : COMERA_OK;
 }
