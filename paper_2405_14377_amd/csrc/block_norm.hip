@@ -48,7 +48,8 @@ struct NormArgs {
 };
 
 // Sums of NV (1, 2 or 4) values over the lanes of a row, the same bits in
-// every lane.  Over a wave: the values are folded into one register, each in
+// every lane of it.  Rows of LPR = 16 or 32 lanes: exchanges within them.
+// Over a wave: the values are folded into one register, each in
 // the rows of 16 lanes of its own, then summed within the rows, which takes
 // 10 instructions for four values (four sums by themselves: about 50).  Rows
 // of several waves: the waves' sums go through one of two LDS buffers in turn
@@ -56,9 +57,18 @@ struct NormArgs {
 // last use has passed), eight lanes read them and exchange them.  Every
 // thread of the workgroup calls it equally often when a row has several
 // waves.
-template <int NV>
+template <int LPR, int NV>
 __device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[8][4], int &turn, int waves) {
     static_assert(NV == 1 || NV == 2 || NV == 4, "one, two or four sums");
+    static_assert(LPR == 0 || LPR == 16 || LPR == 32, "parts of a wave, or whole waves");
+    if constexpr (LPR > 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            v[i] = sum_of_16(v[i]);
+            if constexpr (LPR == 32) v[i] = fold_16(v[i], v[i]);
+        }
+        return;
+    }
     float s;
     if constexpr (NV == 4) {
         s = fold_16(fold_32(v[0], v[1]), fold_32(v[2], v[3]));     // rows: v0, v2, v1, v3
@@ -163,7 +173,7 @@ __device__ __forceinline__ void load_param(const float *p, float otherwise, cons
 // mean and reciprocal root of a row (mean 0 for RMS); two passes over the
 // registers for LAYER, so that no digits are lost where the mean is large.
 // Entries that are not the lane's own are zeros in v.
-template <int VEC, int CH>
+template <int LPR, int VEC, int CH>
 __device__ __forceinline__ void row_stats(const float (&v)[CH * VEC], const Columns<VEC, CH> &k, int kind, float inv_n,
                                           float eps, float (*red)[8][4], int &turn, int waves, float &mean,
                                           float &r) {
@@ -173,7 +183,7 @@ __device__ __forceinline__ void row_stats(const float (&v)[CH * VEC], const Colu
         float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < CH * VEC; ++i) s[0] += v[i];
-        row_sum<1>(s, red, turn, waves);
+        row_sum<LPR>(s, red, turn, waves);
         mean = s[0] * inv_n;
         float d[CH * VEC];
 #pragma unroll
@@ -185,7 +195,7 @@ __device__ __forceinline__ void row_stats(const float (&v)[CH * VEC], const Colu
 #pragma unroll
         for (int i = 0; i < CH * VEC; ++i) q[0] += v[i] * v[i];
     }
-    row_sum<1>(q, red, turn, waves);
+    row_sum<LPR>(q, red, turn, waves);
     r = rsqrtf(q[0] * inv_n + eps);
 }
 
@@ -205,14 +215,16 @@ struct FwdRows {
     }
 };
 
-template <class TS, class TA, int VEC, int CH>
+// LPR: lanes of a row that is a part of a wave; 0 for rows of p.lpr lanes,
+// whole waves.
+template <class TS, class TA, int VEC, int CH, int LPR>
 __global__ __launch_bounds__(512) void block_norm_fwd_kernel(NormArgs p) {
     constexpr int NE = VEC * CH;
     __shared__ __attribute__((aligned(16))) float red[2][8][4];
     int turn = 0;
-    const int waves = p.lpr >> 6, rows = int(blockDim.x) / p.lpr;
-    const int lane = int(threadIdx.x) % p.lpr;
-    const Columns<VEC, CH> k(lane, p.lpr, p.N);
+    const int lpr = LPR ? LPR : p.lpr, waves = lpr >> 6, rows = int(blockDim.x) / lpr;
+    const int lane = int(threadIdx.x) % lpr;
+    const Columns<VEC, CH> k(lane, lpr, p.N);
     const float inv_n = 1.f / float(p.N);
     float pw[NE], pb[NE], w[NE], wb[NE];
     load_param<VEC, CH>(p.gate_ch, 1.f, k, pw);
@@ -227,13 +239,16 @@ __global__ __launch_bounds__(512) void block_norm_fwd_kernel(NormArgs p) {
     }
     load_param<VEC, CH>(p.pre_w, 1.f, k, w);
     load_param<VEC, CH>(p.pre_b, 0.f, k, wb);
+    // every thread takes equally many rows: those behind the last one read
+    // it again and write nothing
     const int64_t step = int64_t(gridDim.x) * rows;
-    int64_t row = int64_t(blockIdx.x) * rows + int(threadIdx.x) / p.lpr;
+    int64_t row = int64_t(blockIdx.x) * rows + int(threadIdx.x) / lpr;
     FwdRows<TS, TA, VEC, CH> next;
     next.load(p, min(row, p.b - 1), k);
-    for (; row < p.b; row += step) {
+    for (int64_t base = int64_t(blockIdx.x) * rows; base < p.b; base += step, row += step) {
+        const bool live = row < p.b;
         const FwdRows<TS, TA, VEC, CH> in = next;
-        if (row + step < p.b) next.load(p, row + step, k);
+        if (base + step < p.b) next.load(p, min(row + step, p.b - 1), k);
         const int64_t at = row * p.N;
         float x[NE];
 #pragma unroll
@@ -245,7 +260,7 @@ __global__ __launch_bounds__(512) void block_norm_fwd_kernel(NormArgs p) {
             k.clear(f);
             float mean = 0.f, r = 1.f;
             if (p.post != COMERA_NORM_NONE)
-                row_stats<VEC, CH>(f, k, p.post, inv_n, p.eps, red, turn, waves, mean, r);
+                row_stats<LPR, VEC, CH>(f, k, p.post, inv_n, p.eps, red, turn, waves, mean, r);
 #pragma unroll
             for (int i = 0; i < NE; ++i) {
                 float z = (f[i] - mean) * r * pw[i] + pb[i];
@@ -256,9 +271,9 @@ __global__ __launch_bounds__(512) void block_norm_fwd_kernel(NormArgs p) {
         k.clear(x);
         // the pre-norm takes Xn before its rounding to the stream's type
         float mean = 0.f, r = 1.f;
-        if (p.pre != COMERA_NORM_NONE) row_stats<VEC, CH>(x, k, p.pre, inv_n, p.eps, red, turn, waves, mean, r);
-        if (p.Xn) store_row<TS, VEC, CH>(p.Xn, at, k, x);
-        if (p.H) {
+        if (p.pre != COMERA_NORM_NONE) row_stats<LPR, VEC, CH>(x, k, p.pre, inv_n, p.eps, red, turn, waves, mean, r);
+        if (p.Xn && live) store_row<TS, VEC, CH>(p.Xn, at, k, x);
+        if (p.H && live) {
 #pragma unroll
             for (int i = 0; i < NE; ++i) x[i] = (x[i] - mean) * r * w[i] + wb[i];
             store_row<TA, VEC, CH>(p.H, at, k, x);
@@ -309,7 +324,7 @@ struct BwdRows {
 // times y_X and of dH.  FULL: means and the sums for biases; without it (RMS
 // norms, no bias) a third of the arithmetic and half of the sums fall away.
 // block_norm_finish_kernel adds the workgroups' sums in order.
-template <class TS, class TA, int VEC, int CH, bool FULL>
+template <class TS, class TA, int VEC, int CH, bool FULL, int LPR>
 __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
     constexpr int NE = VEC * CH, NS = FULL ? 4 : 2;
     // two tokens' rows do not fit the registers with 16 entries a lane, nor with
@@ -318,9 +333,9 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
     __shared__ __attribute__((aligned(16))) float red[2][8][4];
     extern __shared__ float share[];       // [2][rows][N] when rows > 1
     int turn = 0;
-    const int waves = p.lpr >> 6, rows = int(blockDim.x) / p.lpr;
-    const int lane = int(threadIdx.x) % p.lpr;
-    const Columns<VEC, CH> k(lane, p.lpr, p.N);
+    const int lpr = LPR ? LPR : p.lpr, waves = lpr >> 6, rows = int(blockDim.x) / lpr;
+    const int lane = int(threadIdx.x) % lpr;
+    const Columns<VEC, CH> k(lane, lpr, p.N);
     const float inv_n = 1.f / float(p.N);
     const bool pre_mean = FULL && p.dH && p.pre == COMERA_NORM_LAYER;
     const bool post_mean = FULL && p.F && p.post == COMERA_NORM_LAYER;
@@ -340,7 +355,7 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
     // every thread takes equally many rows: those behind the last one read
     // it again and write nothing
     const int64_t step = int64_t(gridDim.x) * rows;
-    int64_t row = int64_t(blockIdx.x) * rows + int(threadIdx.x) / p.lpr;
+    int64_t row = int64_t(blockIdx.x) * rows + int(threadIdx.x) / lpr;
     BwdRows<TS, TA, VEC, CH> next;
     if constexpr (AHEAD) next.load(p, min(row, p.b - 1), k);
     for (int64_t base = int64_t(blockIdx.x) * rows; base < p.b; base += step, row += step) {
@@ -362,7 +377,7 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
                 if (pre_mean) mean[0] += in.x[i / VEC].get(i % VEC);
                 if (post_mean) mean[1] += in.f[i / VEC].get(i % VEC);
             }
-            row_sum<2>(mean, red, turn, waves);
+            row_sum<LPR>(mean, red, turn, waves);
             mean[0] *= inv_n;
             mean[1] *= inv_n;
         }
@@ -388,7 +403,7 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
         if (p.F)
 #pragma unroll
             for (int i = 0; i < NE; ++i) s[3] += f[i] * f[i];
-        if (p.dH || (p.F && p.post != COMERA_NORM_NONE)) row_sum<4>(s, red, turn, waves);
+        if (p.dH || (p.F && p.post != COMERA_NORM_NONE)) row_sum<LPR>(s, red, turn, waves);
 #pragma unroll
         for (int i = 0; i < NE; ++i) t[i] = 0.f;
         if (p.dXn)
@@ -438,7 +453,7 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
             if constexpr (FULL) q[1] += t[i];
         }
         if (p.post != COMERA_NORM_NONE) {
-            row_sum<2>(q, red, turn, waves);
+            row_sum<LPR>(q, red, turn, waves);
             const float sy = q[0] * inv_n, su = post_mean ? q[1] * inv_n : 0.f;
 #pragma unroll
             for (int i = 0; i < NE; ++i) t[i] = r * (FULL ? t[i] - su - f[i] * sy : t[i] - f[i] * sy);
@@ -455,7 +470,7 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
             if ((p.want >> s) & 1) store_row<float, VEC, CH>(out, int64_t(s) * p.N, k, acc[s]);
         return;
     }
-    const int mine = int(threadIdx.x) / p.lpr;
+    const int mine = int(threadIdx.x) / lpr;
 #pragma unroll
     for (int s0 = 0; s0 < NS; s0 += 2) {
         if (!((p.want >> s0) & 3)) continue;
@@ -553,11 +568,20 @@ struct Spread {
     int threads() const { return lpr * rows; }
 };
 
+// Rows of up to 256 columns: 16 or 32 lanes with 8 entries each, several rows
+// a wave.  65536 rows of 64, 100, 256 columns with LAYER norms and a token
+// gate: forward 13.3, 14.0, 32.4 us (a wave each: 35.4, 36.9, 41.8), backward
+// 31.9, 42.6, 75.4 (96.9, 117, 114).  Single entries below 8 columns.
+Spread narrow_spread(int N, int waves) {
+    if (N < 8) return {1, 1, 64, waves};
+    const int lpr = N <= 128 ? 16 : 32;
+    return {8, 1, lpr, 64 * waves / lpr};
+}
+
 // Forward: 8 entries a lane up to 512 columns; above, 12 or 16, whichever
-// leaves fewer idle lanes (768 columns: 64 lanes x 12).  Single entries below
-// 8 columns.
+// leaves fewer idle lanes (768 columns: 64 lanes x 12).
 Spread fwd_spread(int N) {
-    if (N < 8) return {1, 1, 64, kWaveRows};
+    if (N <= 256) return narrow_spread(N, kWaveRows);
     if (N <= 512) return {8, 1, 64, kWaveRows};
     const int l12 = (N + 767) / 768 * 64, l16 = (N + 1023) / 1024 * 64;
     const Spread sp = l12 * 12 < l16 * 16 && l12 <= 512 ? Spread{4, 3, l12, 1} : Spread{8, 2, l16, 1};
@@ -568,9 +592,9 @@ Spread fwd_spread(int N) {
 // so 8 entries a lane as long as eight waves cover the row (4096 columns), 12
 // where one wave then does (up to 768) or eight waves do (up to 6144), and 16
 // above, which read one row at a time: 2048 x 5000 LAYER fp32 with 16 entries
-// and two rows spilled registers (165 us; 54 with 12).
+// and two rows spilled registers (165 us; 50 with 12).
 Spread bwd_spread(int N) {
-    if (N < 8) return {1, 1, 64, kBwdWaves};
+    if (N <= 256) return narrow_spread(N, kBwdWaves);
     if (N > 512 && N <= 768) return {4, 3, 64, kBwdWaves};
     if (N > 6144) return {8, 2, (N + 1023) / 1024 * 64, 1};
     if (N > 4096) return {4, 3, (N + 767) / 768 * 64, 1};
@@ -584,7 +608,7 @@ int64_t bwd_parts(const Spread &sp, int64_t b) {
 
 template <class TS, class TA>
 void launch_fwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
-        // Up to 4096 workgroups, with two rows each at least (four where a row is
+    // Up to 4096 workgroups, with two rows each at least (four where a row is
     // eight waves) so that loads run ahead, but no CU left without its four:
     // 4096 x 8192 fp32 119 us with one row each, 105 with four; 40001 x 1024
     // bf16 81 us with five, 77 with two or three.
@@ -593,13 +617,17 @@ void launch_fwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
         unsigned(std::min<int64_t>(4096, std::max(std::min<int64_t>(groups, 1024), groups / least)));
     const dim3 block(sp.threads());
     if (sp.vec == 1)
-        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 1, 1>), dim3(grid), block, 0, st, p);
+        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 1, 1, 0>), dim3(grid), block, 0, st, p);
     else if (sp.vec == 4)
-        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 4, 3>), dim3(grid), block, 0, st, p);
-    else if (sp.ch == 1)
-        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 8, 1>), dim3(grid), block, 0, st, p);
+        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 4, 3, 0>), dim3(grid), block, 0, st, p);
+    else if (sp.ch == 2)
+        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 8, 2, 0>), dim3(grid), block, 0, st, p);
+    else if (sp.lpr == 16)
+        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 8, 1, 16>), dim3(grid), block, 0, st, p);
+    else if (sp.lpr == 32)
+        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 8, 1, 32>), dim3(grid), block, 0, st, p);
     else
-        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 8, 2>), dim3(grid), block, 0, st, p);
+        COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 8, 1, 0>), dim3(grid), block, 0, st, p);
 }
 
 template <class TS, class TA, bool FULL>
@@ -608,13 +636,17 @@ void launch_bwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
     const dim3 block(sp.threads());
     const size_t lds = sp.rows > 1 ? sizeof(float) * 2 * sp.rows * p.N : 0;
     if (sp.vec == 1)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 1, 1, FULL>), dim3(grid), block, lds, st, p);
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 1, 1, FULL, 0>), dim3(grid), block, lds, st, p);
     else if (sp.vec == 4)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 4, 3, FULL>), dim3(grid), block, lds, st, p);
-    else if (sp.ch == 1)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 1, FULL>), dim3(grid), block, lds, st, p);
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 4, 3, FULL, 0>), dim3(grid), block, lds, st, p);
+    else if (sp.ch == 2)
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 2, FULL, 0>), dim3(grid), block, lds, st, p);
+    else if (sp.lpr == 16)
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 1, FULL, 16>), dim3(grid), block, lds, st, p);
+    else if (sp.lpr == 32)
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 1, FULL, 32>), dim3(grid), block, lds, st, p);
     else
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 2, FULL>), dim3(grid), block, lds, st, p);
+        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 1, FULL, 0>), dim3(grid), block, lds, st, p);
 }
 
 }  // namespace

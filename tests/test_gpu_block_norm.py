@@ -184,8 +184,8 @@ class Case:
                 raise AssertionError(f"{k}: {e}") from None
 
 
-WIDTHS = [1, 2, 5, 7, 8, 9, 63, 64, 100, 511, 512, 513, 767, 768, 769, 1001, 1024, 1025, 1536, 1537, 2048, 3000, 4096,
-          5000, 6144, 6145, 8191, 8192]
+WIDTHS = [1, 2, 5, 7, 8, 9, 63, 64, 100, 127, 128, 129, 255, 256, 257, 511, 512, 513, 767, 768, 769, 1001, 1024, 1025,
+          1536, 1537, 2048, 3000, 4096, 5000, 6144, 6145, 8191, 8192]
 
 
 @pytest.mark.parametrize("types", TYPES, ids="-".join)
@@ -217,7 +217,8 @@ def test_without_a_block_before(n):
         c.check_backward()
 
 
-@pytest.mark.parametrize("b,n", [(1, 768), (255, 512), (256, 100), (1025, 768), (2100, 256), (700, 1536), (3001, 40)])
+@pytest.mark.parametrize("b,n", [(1, 768), (255, 512), (256, 100), (1025, 768), (2100, 256), (700, 1536), (3001, 40),
+                                 (8200, 64), (4111, 136)])
 def test_batches(b, n):
     c = Case(b, n, TYPES[1], "layer", "rms", "channel")
     c.check_forward()

@@ -138,7 +138,7 @@ def test_norm_refusals(checked):
 
 
 def test_norm_launches(checked):
-    for width in (1, 7, 8, 511, 512, 513, 768, 1024, 1025, 1537, 4096, 6144, 6145, 8192):
+    for width in (1, 7, 8, 127, 128, 129, 256, 257, 511, 512, 513, 768, 1024, 1025, 1537, 4096, 6144, 6145, 8192):
         for b in (1, 3, 4, 257, 1025, 70000, 2 ** 33):
             for s in (C.block_norm_shape(width, C.F32, C.F32, C.NORM_LAYER, C.NORM_LAYER, C.GATE_TOKEN),
                       C.block_norm_shape(width, C.BF16, C.BF16, C.NORM_RMS, C.NORM_RMS, C.GATE_CHANNEL)):
