@@ -19,21 +19,24 @@ namespace {
 
 constexpr int kRowsVec = 8;            // columns of a lane
 
-// A wave copies a row, 64 lanes x VEC columns at a time.  The last lane with
+// LPR lanes copy a row, LPR x VEC columns at a time.  The last lane with
 // columns is moved back to end at the row's end (its first entries are
 // written twice with the same values), so E >= VEC.  Bound by HBM: 65536
 // uniform ids of a 50000 x 1536 fp32 table to bf16 94 us, 5.4 TB/s (two or
 // four rows a wave, whose loads are in flight together: 95 and 96 us).
-template <class TT, class TY, int VEC>
+template <class TT, class TY, int VEC, int LPR>
 __global__ __launch_bounds__(256) void dense_rows_kernel(const int64_t *ids, int64_t n, const TT *T, int64_t V,
                                                          int64_t E, float scale, TY *Y, int32_t *err_flag) {
-    const int w = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), lane = threadIdx.x & 63;
-    for (int64_t row = int64_t(blockIdx.x) * 4 + w; row < n; row += int64_t(gridDim.x) * 4) {
+    // one row a wave: its number and its id are uniform
+    const int r = LPR == 64 ? __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6) : int(threadIdx.x) / LPR;
+    const int lane = threadIdx.x % LPR;
+    constexpr int kRows = 256 / LPR;
+    for (int64_t row = int64_t(blockIdx.x) * kRows + r; row < n; row += int64_t(gridDim.x) * kRows) {
         const int64_t id = ids[row];
         const bool in = uint64_t(id) < uint64_t(V);
         if (!in && err_flag && lane == 0) *err_flag = 1;
         const TT *src = T + (in ? id : 0) * E;
-        for (int64_t c0 = lane * VEC; c0 < E; c0 += 64 * VEC) {
+        for (int64_t c0 = lane * VEC; c0 < E; c0 += LPR * VEC) {
             const int64_t c = min(c0, E - VEC);
             Pack<TT, VEC> p;
             p.load(src + c);
@@ -626,18 +629,27 @@ void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L)
 
 comera_status dense_status() { return note_hip(launch_status(), "dense embedding") ? COMERA_ERR_HIP : COMERA_OK; }
 
+template <class TT, class TY, int VEC, int LPR>
+void launch_rows(const comera_dense_embed_shape *s, const int64_t *ids, int64_t n, const void *T, float scale, void *Y,
+                 int32_t *err_flag, hipStream_t st) {
+    constexpr int kRows = 256 / LPR;
+    const dim3 grid(unsigned(std::min<int64_t>((n + kRows - 1) / kRows, 1 << 20)));
+    COMERA_LAUNCH((dense_rows_kernel<TT, TY, VEC, LPR>), grid, dim3(256), 0, st, ids, n, static_cast<const TT *>(T),
+                  s->V, s->E, scale, static_cast<TY *>(Y), err_flag);
+}
+
+// Narrow rows share a wave: 65536 ids of 50000 x 64 7.2 us, 13.1 with a wave each
 template <class TT, class TY>
 void launch_rows(const comera_dense_embed_shape *s, const int64_t *ids, int64_t n, const void *T, float scale, void *Y,
                  int32_t *err_flag, hipStream_t st) {
-    const dim3 grid(unsigned(std::min<int64_t>((n + 3) / 4, 1 << 20)));
-    const TT *t = static_cast<const TT *>(T);
-    TY *y = static_cast<TY *>(Y);
-    if (s->E >= kRowsVec)
-        COMERA_LAUNCH((dense_rows_kernel<TT, TY, kRowsVec>), grid, dim3(256), 0, st, ids, n, t, s->V, s->E, scale, y,
-                      err_flag);
+    if (s->E < kRowsVec)
+        launch_rows<TT, TY, 1, 8>(s, ids, n, T, scale, Y, err_flag, st);
+    else if (s->E <= 16 * kRowsVec)
+        launch_rows<TT, TY, kRowsVec, 16>(s, ids, n, T, scale, Y, err_flag, st);
+    else if (s->E <= 32 * kRowsVec)
+        launch_rows<TT, TY, kRowsVec, 32>(s, ids, n, T, scale, Y, err_flag, st);
     else
-        COMERA_LAUNCH((dense_rows_kernel<TT, TY, 1>), grid, dim3(256), 0, st, ids, n, t, s->V, s->E, scale, y,
-                      err_flag);
+        launch_rows<TT, TY, kRowsVec, 64>(s, ids, n, T, scale, Y, err_flag, st);
 }
 
 template <class TY, class TT, int VEC>

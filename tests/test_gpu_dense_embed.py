@@ -52,7 +52,8 @@ def _check_backward(got, V, ids, dY, scale, pad, table):
 @pytest.mark.parametrize("table", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["f32", "bf16"])
 @pytest.mark.parametrize("V,E,n,offset", [(1, 1, 1, 0), (7, 3, 20, 1), (50, 8, 33, 0), (50, 9, 1, 3),
-                                          (300, 100, 257, 0), (1000, 768, 130, 0), (33, 1001, 65, 1),
+                                          (300, 100, 257, 0), (300, 128, 63, 0), (300, 129, 257, 1),
+                                          (64, 256, 70, 0), (64, 257, 70, 3), (1000, 768, 130, 0), (33, 1001, 65, 1),
                                           (20, 4097, 9, 0)])
 def test_forward(V, E, n, offset, table, act):
     rng = np.random.default_rng(V + E)
