@@ -29,6 +29,10 @@ constexpr int kChunkTensors = 120;     // tensors of one launch whose table is a
 constexpr int kTile = 8192;            // entries that a workgroup takes at a time
 constexpr int kGradThreads = 256;
 constexpr int kGradParts = 2048;       // workgroups of the first pass over all launches, up to twice as many
+// Up to so many tiles one workgroup does both passes: 5 tiles 8.1 us a call
+// (two launches: 9.6), 9 tiles 9.3 (9.6), 18 tiles 15.5 (9.6)
+constexpr uint32_t kSmallTiles = 8;
+constexpr int kSmallThreads = 1024;
 constexpr int kScaleBlocks = 2048;     // workgroups of one launch of the second pass, at most
 // From here on (bytes read and written) the clipped gradients are stored
 // around the last-level cache: their lines would leave it only during the
@@ -94,14 +98,15 @@ __global__ __launch_bounds__(128) void grad_table_kernel(GradChunk c, Entry *tab
     table[threadIdx.x] = x;
 }
 
-// sum over a workgroup of 256 threads in a fixed order, in every thread
+// sum over a workgroup in a fixed order, in every thread
+template <int THREADS = kGradThreads>
 __device__ __forceinline__ double block_sum(double v) {
-    __shared__ double red[kGradThreads / 64];
+    __shared__ double red[THREADS / 64];
     for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     v = 0;
-    for (int w = 0; w < kGradThreads / 64; ++w) v += red[w];
+    for (int w = 0; w < THREADS / 64; ++w) v += red[w];
     return v;
 }
 
@@ -111,7 +116,8 @@ __device__ __forceinline__ double block_sum(double v) {
 template <class T, class Use, class Rest>
 __device__ __forceinline__ void for_tile(const T *g, int64_t at, int64_t n, Use use, Rest rest) {
     constexpr int V = 16 / sizeof(T), U = kTile / (V * kGradThreads);
-    const int64_t i0 = at + int64_t(threadIdx.x) * V;
+    const int tid = threadIdx.x % kGradThreads;        // a small list's workgroup takes several tiles side by side
+    const int64_t i0 = at + int64_t(tid) * V;
     if (at + kTile <= n) {
         Pack<T, V> p[U];
 #pragma unroll
@@ -131,7 +137,7 @@ __device__ __forceinline__ void for_tile(const T *g, int64_t at, int64_t n, Use 
         for (int u = 0; u < U; ++u)
             if (i0 + u * kGradThreads * V < whole) use(p[u], i0 + u * kGradThreads * V);
     }
-    if (whole + threadIdx.x < n) rest(whole + threadIdx.x);
+    if (whole + tid < n) rest(whole + tid);
 }
 
 template <class T>
@@ -207,13 +213,18 @@ __device__ __forceinline__ void tile_scale(const T *g, T *out, int64_t at, int64
         });
 }
 
+// the factor of every entry
+__device__ __forceinline__ float factor(double norm, float scale, float max_norm) {
+    const bool clip = isfinite(float(norm)) && norm > double(max_norm);
+    return clip ? float(double(scale) * (double(max_norm) / norm)) : scale;
+}
+
 template <class List, bool STREAM>
 __global__ __launch_bounds__(kGradThreads) void grad_scale_kernel(List c, const double *part, float scale,
                                                                   float max_norm, float *norm, int32_t *flag) {
     const double v = total_norm(part, c.all_parts, scale);
     if (c.part0 == 0 && blockIdx.x == 0 && threadIdx.x == 0) write_norm(v, norm, flag);
-    const bool clip = isfinite(float(v)) && v > double(max_norm);
-    const float f = clip ? float(double(scale) * (double(max_norm) / v)) : scale;
+    const float f = factor(v, scale, max_norm);
     // from the last tile back: what the first pass read last is still cached
     const uint32_t b = gridDim.x - 1 - blockIdx.x;
     const uint32_t t0 = uint32_t(uint64_t(c.tiles) * b / gridDim.x);
@@ -228,6 +239,33 @@ __global__ __launch_bounds__(kGradThreads) void grad_scale_kernel(List c, const 
             tile_scale<bf16, STREAM>(static_cast<const bf16 *>(x.g), static_cast<bf16 *>(x.out), at, x.size(), f);
         else
             tile_scale<float, STREAM>(static_cast<const float *>(x.g), static_cast<float *>(x.out), at, x.size(), f);
+    }
+}
+
+// A small list's norm and clipping in one launch of one workgroup, four tiles
+// side by side; the second pass reads from the L2.
+__global__ __launch_bounds__(kSmallThreads) void grad_small_kernel(GradChunk c, float scale, float max_norm,
+                                                                   float *norm, int32_t *flag) {
+    constexpr uint32_t kSide = kSmallThreads / kGradThreads;
+    const uint32_t t0 = uint32_t(__builtin_amdgcn_readfirstlane(int(threadIdx.x) / kGradThreads));
+    double s = 0;
+    for (uint32_t t = t0; t < c.tiles; t += kSide) {
+        const Entry x = c.at(tensor_of(c, t));
+        const int64_t at = int64_t(t - x.tile0) * kTile;
+        s += x.is_bf16() ? tile_squares(static_cast<const bf16 *>(x.g), at, x.size())
+                         : tile_squares(static_cast<const float *>(x.g), at, x.size());
+    }
+    const double v = double(scale) * sqrt(block_sum<kSmallThreads>(s));
+    if (threadIdx.x == 0) write_norm(v, norm, flag);
+    const float f = factor(v, scale, max_norm);
+    for (uint32_t t = t0; t < c.tiles; t += kSide) {
+        const Entry x = c.at(tensor_of(c, t));
+        if (f == 1.f && x.out == x.g) continue;
+        const int64_t at = int64_t(t - x.tile0) * kTile;
+        if (x.is_bf16())
+            tile_scale<bf16, false>(static_cast<const bf16 *>(x.g), static_cast<bf16 *>(x.out), at, x.size(), f);
+        else
+            tile_scale<float, false>(static_cast<const float *>(x.g), static_cast<float *>(x.out), at, x.size(), f);
     }
 }
 
@@ -407,6 +445,11 @@ comera_status comera_grad_clip(comera_grad_plan_t p, float scale, float max_norm
     }
     hipStream_t st = hipStream_t(stream);
     double *part = static_cast<double *>(ws);
+    if (p->chunks.size() == 1 && p->chunks[0].tiles <= kSmallTiles) {
+        COMERA_LAUNCH(grad_small_kernel, dim3(1), dim3(kSmallThreads), 0, st, p->chunks[0], scale, max_norm, norm,
+                      flag);
+        return note_hip(launch_status(), "gradient clipping") ? COMERA_ERR_HIP : COMERA_OK;
+    }
     launch_squares(p, part, st);
     if (p->table.e)
         launch_scale(p, p->table, part, scale, max_norm, norm, flag, st);
