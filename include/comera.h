@@ -348,7 +348,7 @@ comera_status comera_tt_embed_backward_ex(const comera_tt_embed_shape *s, const 
  * Around the compressed layers of a training step.  Beside the conventions
  * above, the calls below run on the current device, which must be the one of
  * `stream` and of every buffer; buffers need the alignment of their entries
- * only (workspaces 8 bytes).  A workspace carries nothing from one call to
+ * only (workspaces 16 bytes).  A workspace carries nothing from one call to
  * the next, and calls that may overlap need one each. */
 
 /* An uncompressed embedding table T[V, E], row-major. */

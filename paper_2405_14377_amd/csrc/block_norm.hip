@@ -722,7 +722,7 @@ comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64
     const int64_t parts = bwd_parts(sp, b);
     if (b > 0 && ((!dXn && !dH) || (dH && !Xn))) return COMERA_ERR_INVALID_ARG;
     if (params && b > 0 &&
-        (!ws || ws_bytes < comera_block_norm_workspace_bytes(s, b) || reinterpret_cast<uintptr_t>(ws) % 8))
+        (!ws || ws_bytes < comera_block_norm_workspace_bytes(s, b) || reinterpret_cast<uintptr_t>(ws) % 16))
         return COMERA_ERR_WORKSPACE;
     hipStream_t st = hipStream_t(stream);
     const bool full = dpost_b || dpre_b || (channel && dgate && post_b) || s->pre == COMERA_NORM_LAYER ||

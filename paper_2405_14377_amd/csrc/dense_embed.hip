@@ -64,7 +64,7 @@ struct GroupArgs {
     int lg, Q;
     int parts;          // the tokens are walked in so many parts, by workgroups of their own
     uint32_t few;       // an id with more tokens goes to the list of long ones
-    uint2 *order;       // (token, id) by id
+    uint4 *order;       // (token, id, first place and tokens of the id) by id
     uint2 *range;       // (first place, tokens) of each id
     uint4 *many;        // [workgroup][most_many] its long ids, (id, first place, tokens, 0)
     int most_many;
@@ -148,8 +148,8 @@ __device__ __forceinline__ uint32_t walk(const GroupArgs &a, int64_t s0, int64_t
 // Puts 64 owned tokens (those lanes with `own`) to their places: lanes of one
 // id are ranked by their lane number, their first lane moves the id's place
 // on.  Every id bit halves the set of lanes that agree with this one.
-__device__ __forceinline__ void put_tokens(const GroupArgs &a, volatile uint32_t *place, bool own, uint64_t token_id,
-                                           uint32_t lane) {
+__device__ __forceinline__ void put_tokens(const GroupArgs &a, volatile uint32_t *place, const uint2 *ids, bool own,
+                                           uint64_t token_id, uint32_t lane) {
     const uint32_t q = uint32_t(token_id) >> a.lg;
     uint64_t same = __ballot(own);
 #pragma unroll
@@ -160,17 +160,17 @@ __device__ __forceinline__ void put_tokens(const GroupArgs &a, volatile uint32_t
     if (own) {
         const uint32_t rank = bits_below(same);
         const uint32_t first = place[q];
-        a.order[first + rank] = make_uint2(uint32_t(token_id >> 32), uint32_t(token_id));
+        a.order[first + rank] = make_uint4(uint32_t(token_id >> 32), uint32_t(token_id), ids[q].x, ids[q].y);
         if (rank == 0) place[q] = first + uint32_t(__popcll(same));
     }
 }
 
 // the first `n` tokens of a wave's list
-__device__ __forceinline__ void put_list(const GroupArgs &a, volatile uint32_t *place, const volatile uint64_t *list,
-                                         uint32_t n, uint32_t lane) {
+__device__ __forceinline__ void put_list(const GroupArgs &a, volatile uint32_t *place, const uint2 *ids,
+                                         const volatile uint64_t *list, uint32_t n, uint32_t lane) {
     for (uint32_t i = 0; i < n; i += 64) {
         const bool own = i + lane < n;
-        put_tokens(a, place, own, own ? list[i + lane] : 0, lane);
+        put_tokens(a, place, ids, own, own ? list[i + lane] : 0, lane);
     }
 }
 
@@ -212,6 +212,7 @@ __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a)
     extern __shared__ uint32_t cnt[];                  // [kGroupWaves][Q]
     __shared__ uint32_t wsum[kGroupWaves], wbelow[kGroupWaves], longs;
     __shared__ uint64_t lists[kGroupWaves][kGroupList];            // token << 32 | id
+    __shared__ uint2 ids[kGroupQ];                     // first place and tokens of the workgroup's ids
     const int t = threadIdx.x, w = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, Q = a.Q;
     const uint32_t groups = gridDim.x, g = blockIdx.x, p = blockIdx.y, all = groups * a.parts;
     for (int i = t; i < kGroupWaves * Q; i += kGroupThreads) cnt[i] = 0;
@@ -260,6 +261,7 @@ __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a)
         if (x < w) base += wsum[x];
     }
     if (t < Q) {
+        ids[t] = make_uint2(base, whole);
         if (p == 0) {
             const int64_t id = (int64_t(t) << a.lg) + g;
             if (id < a.V) a.range[id] = make_uint2(base, whole);
@@ -283,12 +285,12 @@ __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a)
         walk(a, seg.s0, seg.s1, lane, g, [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
             append(own, m, token, id);
             if (listed > kGroupList - 64) {
-                put_list(a, place, list, listed, lane);
+                put_list(a, place, ids, list, listed, lane);
                 listed = 0;
             }
         });
     }
-    put_list(a, place, list, listed, lane);
+    put_list(a, place, ids, list, listed, lane);
     // ids out of range: every workgroup looks at its share of the tokens
     if (a.err_flag)
         for (int64_t at = int64_t(p * groups + g) * kGroupThreads + t; at < a.n; at += int64_t(all) * kGroupThreads)
@@ -302,12 +304,14 @@ constexpr int kFillIds = 64;           // ids of one workgroup that writes zeros
 
 struct SumArgs {
     const void *dY;
-    int64_t V, E;
+    int64_t n, V, E;
+    int64_t jobs;       // chunks times slices
     int slices;         // column slices of a row: 64 lanes x VEC columns
     int lgC;            // log2 of the places of one chunk
     uint32_t few;       // tokens of an id that one wave adds alone
     float scale;
-    const uint2 *order, *range;
+    const uint4 *order;
+    const uint2 *range;
     const uint4 *many;
     const uint32_t *n_many, *total;
     int most_many;
@@ -324,14 +328,13 @@ struct SumArgs {
 // it goes on, for dense_finish_kernel.  Chunks of equal length keep every
 // wave busy alike however the ids are distributed.
 template <class TY, class TT, int VEC>
-__device__ __forceinline__ void sum_chunk(const SumArgs &a, int64_t chunk, int slice, uint32_t nv) {
+__device__ __forceinline__ void sum_chunk(const SumArgs &a, int64_t chunk, int slice, const uint4 &me, uint32_t nv) {
     const int lane = threadIdx.x & 63, C = 1 << a.lgC;
     const int64_t E = a.E, p0 = chunk << a.lgC, c0 = int64_t(slice) * (64 * VEC) + lane * VEC;
     const bool on = c0 < E;
     const int64_t c = on ? min(c0, E - VEC) : 0;
     const bool here = p0 + lane < nv;
-    const uint2 me = here ? a.order[p0 + lane] : make_uint2(0, 0);
-    const uint2 rg = here ? a.range[me.y] : make_uint2(0, 0);
+    const uint2 rg = here ? make_uint2(me.z, me.w) : make_uint2(0, 0);
     const uint32_t pos = uint32_t(p0) + lane;
     const bool few = rg.y <= a.few;
     const bool mine = here && (few ? rg.x >= uint32_t(p0) && rg.x < uint32_t(p0) + C : lane < C);
@@ -388,10 +391,11 @@ __global__ __launch_bounds__(256) void dense_sum_kernel(SumArgs a) {
     const int w = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), lane = threadIdx.x & 63;
     if (blockIdx.x < a.sum_blocks) {
         const uint32_t nv = *a.total;
-        const int64_t jobs = ((int64_t(nv) + (1 << a.lgC) - 1) >> a.lgC) * a.slices;
-        for (int64_t job = int64_t(blockIdx.x) * 4 + w; job < jobs; job += int64_t(a.sum_blocks) * 4) {
+        for (int64_t job = int64_t(blockIdx.x) * 4 + w; job < a.jobs; job += int64_t(a.sum_blocks) * 4) {
             const int64_t chunk = job / a.slices;
-            sum_chunk<TY, TT, VEC>(a, chunk, int(job - chunk * a.slices), nv);
+            // places behind the grouped tokens hold anything and are not used
+            const uint4 me = a.order[min((chunk << a.lgC) + lane, a.n - 1)];
+            if ((chunk << a.lgC) < nv) sum_chunk<TY, TT, VEC>(a, chunk, int(job - chunk * a.slices), me, nv);
         }
         return;
     }
@@ -612,7 +616,7 @@ void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L)
     // an id that begins at a chunk's last place ends within the 64 lanes
     L.few = std::min(64 - (1 << L.lgC), 1 << L.lgC);
     L.chunks = (n + (1 << L.lgC) - 1) >> L.lgC;
-    L.order = take(8 * size_t(n));
+    L.order = take(16 * size_t(n));
     L.range = take(8 * size_t(s->V));
     L.most_many = int(std::min<int64_t>(L.Q, n / L.few + 1));
     L.many = take(16 * size_t(L.most_many) * size_t(L.groups()));
@@ -665,7 +669,8 @@ void launch_sum(const GroupArgs &ga, SumArgs a, const DenseLayout_ &L, hipStream
     COMERA_LAUNCH(dense_group_kernel, grid, dim3(kGroupThreads), size_t(4) * kGroupWaves * L.Q, st, ga);
     // workgroups up to 2^20 of each kind; the kernels walk on from there
     constexpr int64_t kMost = 1 << 20;
-    a.sum_blocks = uint32_t(std::min(kMost, (L.chunks * a.slices + 3) / 4));
+    a.jobs = L.chunks * a.slices;
+    a.sum_blocks = uint32_t(std::min(kMost, (a.jobs + 3) / 4));
     const uint32_t fill = uint32_t(std::min(kMost, (a.V + kFillIds - 1) / kFillIds));
     COMERA_LAUNCH((dense_sum_kernel<TY, TT, VEC>), dim3(a.sum_blocks + fill), dim3(256), 0, st, a);
     COMERA_LAUNCH((dense_finish_kernel<TT, VEC>),
@@ -724,7 +729,7 @@ comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, con
     if (!dT || (n_tokens > 0 && (!ids || !dY))) return COMERA_ERR_INVALID_ARG;
     DenseLayout_ L{};
     dense_layout(s, n_tokens, L);
-    if (!ws || ws_bytes < L.bytes || reinterpret_cast<uintptr_t>(ws) % 8) return COMERA_ERR_WORKSPACE;
+    if (!ws || ws_bytes < L.bytes || reinterpret_cast<uintptr_t>(ws) % 16) return COMERA_ERR_WORKSPACE;
     char *base = static_cast<char *>(ws);
     hipStream_t st = hipStream_t(stream);
     GroupArgs ga{};
@@ -735,7 +740,7 @@ comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, con
     ga.lg = L.lg;
     ga.Q = L.Q;
     ga.few = uint32_t(L.few);
-    ga.order = reinterpret_cast<uint2 *>(base + L.order);
+    ga.order = reinterpret_cast<uint4 *>(base + L.order);
     ga.range = reinterpret_cast<uint2 *>(base + L.range);
     ga.many = reinterpret_cast<uint4 *>(base + L.many);
     ga.most_many = L.most_many;
@@ -747,6 +752,7 @@ comera_status comera_dense_embed_backward(const comera_dense_embed_shape *s, con
     ga.err_flag = err_flag;
     SumArgs a{};
     a.dY = dY;
+    a.n = n_tokens;
     a.V = s->V;
     a.E = s->E;
     a.lgC = L.lgC;

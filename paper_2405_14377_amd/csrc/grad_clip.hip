@@ -294,7 +294,7 @@ struct Range {
 
 comera_status grad_args(comera_grad_plan_t p, float scale, const void *ws, size_t ws_bytes) {
     if (!p || !std::isfinite(scale) || !(scale > 0.f)) return COMERA_ERR_INVALID_ARG;
-    if (!ws || ws_bytes < comera_grad_workspace_bytes(p) || reinterpret_cast<uintptr_t>(ws) % sizeof(double))
+    if (!ws || ws_bytes < comera_grad_workspace_bytes(p) || reinterpret_cast<uintptr_t>(ws) % 16)
         return COMERA_ERR_WORKSPACE;
     return COMERA_OK;
 }

@@ -53,7 +53,7 @@ def test_embed_refusals(checked):
     assert bwd(pad=-2) == C.ERR_INVALID_ARG and bwd(pad=100) == C.ERR_INVALID_ARG and bwd(pad=99) == C.OK
     need = C.comera_dense_embed_workspace_bytes(s, 4)
     assert bwd(ws=None) == C.ERR_WORKSPACE and bwd(w=need - 1) == C.ERR_WORKSPACE and bwd(w=need) == C.OK
-    assert bwd(ws=FAKE + 4) == C.ERR_WORKSPACE
+    assert bwd(ws=FAKE + 8) == C.ERR_WORKSPACE
     assert all(C.comera_dense_embed_workspace_bytes(b, 4) == 0 for b in bad)
     assert C.comera_dense_embed_workspace_bytes(s, -1) == 0
     # no tokens: nothing to read; the gradient is still written
@@ -131,7 +131,7 @@ def test_norm_refusals(checked):
     # the workspace, needed only for the parameters' gradients
     need = C.comera_block_norm_workspace_bytes(shape(64), 10)
     assert _norm_calls(ws=None)[1] == ws and _norm_calls(w=need - 1)[1] == ws and _norm_calls(w=need)[1] == ok
-    assert _norm_calls(ws=FAKE + 4)[1] == ws
+    assert _norm_calls(ws=FAKE + 8)[1] == ws
     assert _norm_calls(ws=None, w=0, dgate=None, dpost_w=None, dpost_b=None, dpre_w=None, dpre_b=None)[1] == ok
     # empty batches
     assert _norm_calls(b=0, X=None, F=None, gate=None, Xn=None, H=None, dXn=None, dH=None, ws=None, w=0) == (ok, ok)
@@ -173,7 +173,7 @@ def test_grad_refusals(checked):
         for scale in (0.0, -1.0, math.inf, math.nan):
             assert call(scale=scale) == bad
         assert call(ws=None) == C.ERR_WORKSPACE and call(w=need - 1) == C.ERR_WORKSPACE
-        assert call(ws=FAKE + 4) == C.ERR_WORKSPACE
+        assert call(ws=FAKE + 8) == C.ERR_WORKSPACE
     assert norm(out=None, flag=None) == bad and clip(out=None, flag=None) == C.OK
     assert clip(most=-1.0) == bad and clip(most=math.nan) == bad and clip(most=math.inf) == C.OK
     C.comera_grad_plan_destroy(p)
