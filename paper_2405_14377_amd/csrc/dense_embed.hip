@@ -145,10 +145,15 @@ __device__ __forceinline__ uint32_t walk(const GroupArgs &a, int64_t s0, int64_t
     return below;
 }
 
+// What the lanes of a wave hand each other through LDS without a barrier, by
+// an LDS address: volatile accesses by a generic one stay flat instructions.
+typedef volatile __attribute__((address_space(3))) uint32_t LdsWord;
+typedef volatile __attribute__((address_space(3))) uint64_t LdsPair;
+
 // Puts 64 owned tokens (those lanes with `own`) to their places: lanes of one
 // id are ranked by their lane number, their first lane moves the id's place
 // on.  Every id bit halves the set of lanes that agree with this one.
-__device__ __forceinline__ void put_tokens(const GroupArgs &a, volatile uint32_t *place, const uint2 *ids, bool own,
+__device__ __forceinline__ void put_tokens(const GroupArgs &a, LdsWord *place, const uint2 *ids, bool own,
                                            uint64_t token_id, uint32_t lane) {
     const uint32_t q = uint32_t(token_id) >> a.lg;
     uint64_t same = __ballot(own);
@@ -166,8 +171,8 @@ __device__ __forceinline__ void put_tokens(const GroupArgs &a, volatile uint32_t
 }
 
 // the first `n` tokens of a wave's list
-__device__ __forceinline__ void put_list(const GroupArgs &a, volatile uint32_t *place, const uint2 *ids,
-                                         const volatile uint64_t *list, uint32_t n, uint32_t lane) {
+__device__ __forceinline__ void put_list(const GroupArgs &a, LdsWord *place, const uint2 *ids,
+                                         const LdsPair *list, uint32_t n, uint32_t lane) {
     for (uint32_t i = 0; i < n; i += 64) {
         const bool own = i + lane < n;
         put_tokens(a, place, ids, own, own ? list[i + lane] : 0, lane);
@@ -219,7 +224,7 @@ __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a)
     if (t == 0) longs = 0;
     __syncthreads();
     const Segment seg(a, int(p), w);
-    volatile uint64_t *list = lists[w];
+    LdsPair *list = (LdsPair *)lists[w];
     uint32_t listed = 0;
     auto append = [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
         const uint32_t i = listed + bits_below(m);
@@ -279,7 +284,7 @@ __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a)
     if (g == groups - 1 && p == 0 && t == kGroupThreads - 1) *a.total = base + whole;
     __syncthreads();
     if (t == 0 && p == 0) a.n_many[g] = longs;
-    volatile uint32_t *place = cnt + w * Q;            // this wave's places
+    LdsWord *place = (LdsWord *)(cnt + w * Q);            // this wave's places
     if (listed > kGroupList) {
         listed = 0;
         walk(a, seg.s0, seg.s1, lane, g, [&](bool own, uint64_t m, uint32_t token, uint32_t id) {
