@@ -19,24 +19,13 @@ struct bf16 {
 template <int BYTES, int ALIGN>
 struct Wide;
 
-// Rows and tensors lie in global memory.  Where an address comes out of a
-// table the compiler cannot tell and takes flat instructions, which count as
-// LDS accesses too and are waited for all at once.
-template <class W>
-using Global = __attribute__((address_space(1))) W;
-
-template <class W, class T>
-__device__ __forceinline__ W load_wide(const T *p) {
-    return *(const Global<W> *)(p);
-}
-
 // a store that leaves no line in the caches (STREAM), or an ordinary one
 template <bool STREAM, class W, class T>
 __device__ __forceinline__ void store_wide(T *p, const W &u) {
     if constexpr (STREAM)
-        __builtin_nontemporal_store(u, (Global<W> *)(p));
+        __builtin_nontemporal_store(u, reinterpret_cast<W *>(p));
     else
-        *(Global<W> *)(p) = u;
+        *reinterpret_cast<W *>(p) = u;
 }
 
 template <>
@@ -73,13 +62,13 @@ struct Pack<float, V> {
         if constexpr (V % 4 == 0) {
 #pragma unroll
             for (int i = 0; i < V; i += 4) {
-                const auto u = load_wide<typename Wide<16, 4>::type>(p + i);
+                const auto u = *reinterpret_cast<const typename Wide<16, 4>::type *>(p + i);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[i + e] = __uint_as_float(u[e]);
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = load_wide<float>(p + i);
+            for (int i = 0; i < V; ++i) x[i] = p[i];
         }
     }
     __device__ __forceinline__ float get(int i) const { return x[i]; }
@@ -99,7 +88,7 @@ struct Pack<float, V> {
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) store_wide<false>(p + i, v[i]);
+            for (int i = 0; i < V; ++i) p[i] = v[i];
         }
     }
 };
@@ -111,20 +100,20 @@ struct Pack<bf16, V> {
         if constexpr (V % 8 == 0) {
 #pragma unroll
             for (int i = 0; i < V; i += 8) {
-                const auto u = load_wide<typename Wide<16, 2>::type>(p + i);
+                const auto u = *reinterpret_cast<const typename Wide<16, 2>::type *>(p + i);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[i / 2 + e] = u[e];
             }
         } else if constexpr (V % 4 == 0) {
 #pragma unroll
             for (int i = 0; i < V; i += 4) {
-                const auto u = load_wide<typename Wide<8, 2>::type>(p + i);
+                const auto u = *reinterpret_cast<const typename Wide<8, 2>::type *>(p + i);
                 x[i / 2] = u[0];
                 x[i / 2 + 1] = u[1];
             }
         } else {
             static_assert(V == 1, "bf16 packs of 1, or of a multiple of 4");
-            x[0] = load_wide<uint16_t>(p);
+            x[0] = p->bits;
         }
     }
     __device__ __forceinline__ float get(int i) const { return i & 1 ? hi_bf16(x[i / 2]) : lo_bf16(x[i / 2]); }
@@ -152,7 +141,7 @@ struct Pack<bf16, V> {
                 store_wide<STREAM>(p + i, u);
             }
         } else {
-            store_wide<false>(p, uint16_t(pack_bf16(v[0], 0.f)));
+            p->bits = uint16_t(pack_bf16(v[0], 0.f));
         }
     }
 };
