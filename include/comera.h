@@ -462,8 +462,9 @@ typedef struct comera_grad_plan_s *comera_grad_plan_t;
  * norm weights: any number and size) for the calls below.  Host only; the
  * plan holds the addresses, which have to stay valid while it is used.  Only
  * comera_grad_plan_set_table changes it, so it may be used from several
- * streams if each has its own workspace.  No two buffers of the list may overlap (INVALID_ARG), nor be
- * misaligned for their dtype.  Release with comera_grad_plan_destroy. */
+ * streams if each has its own workspace.  No two buffers of the list may
+ * overlap (INVALID_ARG), nor be misaligned for their dtype.  Release with
+ * comera_grad_plan_destroy. */
 comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count, comera_grad_plan_t *out);
 void comera_grad_plan_destroy(comera_grad_plan_t p);
 

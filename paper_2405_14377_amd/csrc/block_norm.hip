@@ -47,6 +47,28 @@ struct NormArgs {
     float eps, a, beta;
 };
 
+// The parameters' gradients, from the sums of all workgroups.
+struct FinishArgs {
+    const float *part;
+    int parts, N, want;
+    const float *gate_ch, *post_w, *post_b;
+    float beta;
+    float *dgate, *dpost_w, *dpost_b, *dpre_w, *dpre_b;
+
+    // at column c, from the sums of y_F times T and of T
+    __device__ __forceinline__ void post(int c, float yt, float t) const {
+        const float gate = gate_ch ? gate_ch[c] : 1.f;
+        if (dpost_w) dpost_w[c] = beta * gate * yt;
+        if (dpost_b) dpost_b[c] = beta * gate * t;
+        if (dgate) dgate[c] = beta * (yt * (post_w ? post_w[c] : 1.f) + (post_b ? post_b[c] * t : 0.f));
+    }
+    // of dH times y_X and of dH
+    __device__ __forceinline__ void pre(int c, float yh, float h) const {
+        if (dpre_w) dpre_w[c] = yh;
+        if (dpre_b) dpre_b[c] = h;
+    }
+};
+
 // Sums of NV (1, 2 or 4) values over the lanes of a row, the same bits in
 // every lane of it.  Rows of LPR = 16 or 32 lanes: exchanges within them.
 // Over a wave: the values are folded into one register, each in
@@ -323,9 +345,11 @@ struct BwdRows {
 // of a workgroup: of y_F times T (times the token's gate), of T alike, of dH
 // times y_X and of dH.  FULL: means and the sums for biases; without it (RMS
 // norms, no bias) a third of the arithmetic and half of the sums fall away.
-// block_norm_finish_kernel adds the workgroups' sums in order.
-template <class TS, class TA, int VEC, int CH, bool FULL, int LPR>
-__global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
+// block_norm_finish_kernel adds the workgroups' sums in order; a workgroup
+// that is alone forms the gradients from its own.
+// More arguments: FinishArgs of a workgroup that is alone, or none.
+template <class TS, class TA, int VEC, int CH, bool FULL, int LPR, class... Alone>
+__global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p, Alone... alone) {
     constexpr int NE = VEC * CH, NS = FULL ? 4 : 2;
     // two tokens' rows do not fit the registers with 16 entries a lane, nor with
     // 12 in fp32 and every sum (4096 x 768 LAYER: 27.4 us with spills, 20.0)
@@ -468,33 +492,37 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p) {
 #pragma unroll
         for (int s = 0; s < NS; ++s)
             if ((p.want >> s) & 1) store_row<float, VEC, CH>(out, int64_t(s) * p.N, k, acc[s]);
-        return;
-    }
-    const int mine = int(threadIdx.x) / lpr;
+    } else {
+        const int mine = int(threadIdx.x) / lpr;
 #pragma unroll
-    for (int s0 = 0; s0 < NS; s0 += 2) {
-        if (!((p.want >> s0) & 3)) continue;
+        for (int s0 = 0; s0 < NS; s0 += 2) {
+            if (!((p.want >> s0) & 3)) continue;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) store_row<float, VEC, CH>(share, int64_t(s * rows + mine) * p.N, k, acc[s0 + s]);
-        __syncthreads();
-        for (int c = threadIdx.x; c < 2 * p.N; c += int(blockDim.x)) {
-            const int s = c >= p.N, col = c - s * p.N;
-            const float *x = share + s * rows * p.N + col;
-            float v = x[0];
-            for (int r = 1; r < rows; ++r) v += x[r * p.N];
-            out[int64_t(s0 + s) * p.N + col] = v;
+            for (int s = 0; s < 2; ++s)
+                store_row<float, VEC, CH>(share, int64_t(s * rows + mine) * p.N, k, acc[s0 + s]);
+            __syncthreads();
+            for (int c = threadIdx.x; c < 2 * p.N; c += int(blockDim.x)) {
+                const int s = c >= p.N, col = c - s * p.N;
+                const float *x = share + s * rows * p.N + col;
+                float v = x[0];
+                for (int r = 1; r < rows; ++r) v += x[r * p.N];
+                out[int64_t(s0 + s) * p.N + col] = v;
+            }
+            __syncthreads();
         }
+    }
+    if constexpr (sizeof...(Alone) > 0) {
         __syncthreads();
+        for (int c = threadIdx.x; c < p.N; c += int(blockDim.x)) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};         // sums that are not asked for stay zeros
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+                if ((p.want >> s) & 1) v[FULL ? s : 2 * s] = out[int64_t(s) * p.N + c];
+            (alone.post(c, v[0], v[1]), ...);
+            (alone.pre(c, v[2], v[3]), ...);
+        }
     }
 }
-
-struct FinishArgs {
-    const float *part;
-    int parts, N, want;
-    const float *gate_ch, *post_w, *post_b;
-    float beta;
-    float *dgate, *dpost_w, *dpost_b, *dpre_w, *dpre_b;
-};
 
 constexpr int kFinCols = 32, kFinGroups = 32;
 
@@ -535,16 +563,10 @@ __global__ __launch_bounds__(kFinCols *kFinGroups) void block_norm_finish_kernel
     __syncthreads();
     if (g != 0 || c >= a.N) return;        // ... and group 0 forms the gradients
     const float first = red[0][0][l], second = NP == 2 ? red[NP - 1][0][l] : 0.f;
-    if (blockIdx.y == 0) {                 // of y_F times T, of T
-        const float gate = a.gate_ch ? a.gate_ch[c] : 1.f;
-        if (a.dpost_w) a.dpost_w[c] = a.beta * gate * first;
-        if (a.dpost_b) a.dpost_b[c] = a.beta * gate * second;
-        if (a.dgate)
-            a.dgate[c] = a.beta * (first * (a.post_w ? a.post_w[c] : 1.f) + (a.post_b ? a.post_b[c] * second : 0.f));
-    } else {                               // of dH times y_X, of dH
-        if (a.dpre_w) a.dpre_w[c] = first;
-        if (a.dpre_b) a.dpre_b[c] = second;
-    }
+    if (blockIdx.y == 0)
+        a.post(c, first, second);
+    else
+        a.pre(c, first, second);
 }
 
 // ---------------------------------------------------------------- host side
@@ -602,8 +624,15 @@ Spread bwd_spread(int N) {
     return {8, 1, 64 * waves, kBwdWaves / waves};
 }
 
-int64_t bwd_parts(const Spread &sp, int64_t b) {
-    return std::min<int64_t>((b + sp.rows - 1) / sp.rows, kMaxParts);
+// One workgroup that takes up to two turns forms the parameters' gradients
+// itself: a call on 8 rows of 768 columns with bf16 RMS 13.9 -> 11.0 us, on 16
+// 13.8 -> 11.0, on 16 with LAYER 14.4 -> 15.0; four turns: on 32 12.8, with
+// LAYER 22.5.  Not above 4096 columns: one row of 8192 13.6 -> 14.9, with
+// LAYER 14.4 -> 20.1.
+bool bwd_alone(const Spread &sp, int N, int64_t b) { return b > 0 && b <= 2 * sp.rows && N <= 4096; }
+
+int64_t bwd_parts(const Spread &sp, int N, int64_t b) {
+    return bwd_alone(sp, N, b) ? 1 : std::min<int64_t>((b + sp.rows - 1) / sp.rows, kMaxParts);
 }
 
 template <class TS, class TA>
@@ -630,23 +659,24 @@ void launch_fwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
         COMERA_LAUNCH((block_norm_fwd_kernel<TS, TA, 8, 1, 0>), dim3(grid), block, 0, st, p);
 }
 
-template <class TS, class TA, bool FULL>
-void launch_bwd(const NormArgs &p, const Spread &sp, hipStream_t st) {
-    const unsigned grid = unsigned(bwd_parts(sp, p.b));
+template <class TS, class TA, bool FULL, class... Alone>
+void launch_bwd(const NormArgs &p, const Spread &sp, hipStream_t st, const Alone &...alone) {
+    const unsigned grid = unsigned(bwd_parts(sp, p.N, p.b));
     const dim3 block(sp.threads());
     const size_t lds = sp.rows > 1 ? sizeof(float) * 2 * sp.rows * p.N : 0;
+    auto launch = [&](auto kernel) { COMERA_LAUNCH(kernel, dim3(grid), block, lds, st, p, alone...); };
     if (sp.vec == 1)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 1, 1, FULL, 0>), dim3(grid), block, lds, st, p);
+        launch(block_norm_bwd_kernel<TS, TA, 1, 1, FULL, 0, Alone...>);
     else if (sp.vec == 4)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 4, 3, FULL, 0>), dim3(grid), block, lds, st, p);
-    else if (sp.ch == 2)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 2, FULL, 0>), dim3(grid), block, lds, st, p);
-    else if (sp.lpr == 16)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 1, FULL, 16>), dim3(grid), block, lds, st, p);
-    else if (sp.lpr == 32)
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 1, FULL, 32>), dim3(grid), block, lds, st, p);
-    else
-        COMERA_LAUNCH((block_norm_bwd_kernel<TS, TA, 8, 1, FULL, 0>), dim3(grid), block, lds, st, p);
+        launch(block_norm_bwd_kernel<TS, TA, 4, 3, FULL, 0, Alone...>);
+    else if (sp.ch == 1 && sp.lpr == 16)
+        launch(block_norm_bwd_kernel<TS, TA, 8, 1, FULL, 16, Alone...>);
+    else if (sp.ch == 1 && sp.lpr == 32)
+        launch(block_norm_bwd_kernel<TS, TA, 8, 1, FULL, 32, Alone...>);
+    else if (sp.ch == 1)
+        launch(block_norm_bwd_kernel<TS, TA, 8, 1, FULL, 0, Alone...>);
+    else if constexpr (sizeof...(Alone) == 0)
+        launch(block_norm_bwd_kernel<TS, TA, 8, 2, FULL, 0>);
 }
 
 }  // namespace
@@ -658,7 +688,7 @@ extern "C" {
 
 size_t comera_block_norm_workspace_bytes(const comera_block_norm_shape *s, int64_t b) {
     if (!norm_shape_ok(s) || !norm_supported(s) || b < 0) return 0;
-    return sizeof(float) * 4 * size_t(s->width) * size_t(std::max<int64_t>(1, bwd_parts(bwd_spread(int(s->width)), b)));
+    return sizeof(float) * 4 * size_t(s->width) * size_t(std::max<int64_t>(1, bwd_parts(bwd_spread(int(s->width)), int(s->width), b)));
 }
 
 comera_status comera_block_norm_forward(const comera_block_norm_shape *s, int64_t b, const void *X, const void *F,
@@ -719,7 +749,7 @@ comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64
         return COMERA_ERR_INVALID_ARG;
     const bool params = dpost_w || dpost_b || dpre_w || dpre_b || (channel && dgate);
     const Spread sp = bwd_spread(int(s->width));
-    const int64_t parts = bwd_parts(sp, b);
+    const int64_t parts = bwd_parts(sp, int(s->width), b);
     if (b > 0 && ((!dXn && !dH) || (dH && !Xn))) return COMERA_ERR_INVALID_ARG;
     if (params && b > 0 &&
         (!ws || ws_bytes < comera_block_norm_workspace_bytes(s, b) || reinterpret_cast<uintptr_t>(ws) % 16))
@@ -754,29 +784,39 @@ comera_status comera_block_norm_backward(const comera_block_norm_shape *s, int64
     p.a = s->res_scale;
     p.beta = s->branch_scale;
     p.lpr = sp.lpr;
+    FinishArgs f{};
+    f.part = p.part;
+    f.parts = int(parts);
+    f.N = p.N;
+    f.want = p.want;
+    f.gate_ch = p.gate_ch;
+    f.post_w = post_w;
+    f.post_b = post_b;
+    f.beta = p.beta;
+    f.dgate = channel ? static_cast<float *>(dgate) : nullptr;
+    f.dpost_w = dpost_w;
+    f.dpost_b = dpost_b;
+    f.dpre_w = dpre_w;
+    f.dpre_b = dpre_b;
+    const bool alone = params && bwd_alone(sp, p.N, b);
     if (b > 0 && (params || dX || dF || p.dgate)) {
-        if (s->stream == COMERA_F32 && s->act == COMERA_F32)
-            full ? launch_bwd<float, float, true>(p, sp, st) : launch_bwd<float, float, false>(p, sp, st);
-        else if (s->stream == COMERA_F32)
-            full ? launch_bwd<float, bf16, true>(p, sp, st) : launch_bwd<float, bf16, false>(p, sp, st);
+        auto launch = [&](const auto &...in_it) {
+            if (s->stream == COMERA_F32 && s->act == COMERA_F32)
+                full ? launch_bwd<float, float, true>(p, sp, st, in_it...)
+                     : launch_bwd<float, float, false>(p, sp, st, in_it...);
+            else if (s->stream == COMERA_F32)
+                full ? launch_bwd<float, bf16, true>(p, sp, st, in_it...)
+                     : launch_bwd<float, bf16, false>(p, sp, st, in_it...);
+            else
+                full ? launch_bwd<bf16, bf16, true>(p, sp, st, in_it...)
+                     : launch_bwd<bf16, bf16, false>(p, sp, st, in_it...);
+        };
+        if (alone)
+            launch(f);
         else
-            full ? launch_bwd<bf16, bf16, true>(p, sp, st) : launch_bwd<bf16, bf16, false>(p, sp, st);
+            launch();
     }
-    if (params) {
-        FinishArgs f{};
-        f.part = p.part;
-        f.parts = int(parts);
-        f.N = p.N;
-        f.want = p.want;
-        f.gate_ch = p.gate_ch;
-        f.post_w = post_w;
-        f.post_b = post_b;
-        f.beta = p.beta;
-        f.dgate = channel ? static_cast<float *>(dgate) : nullptr;
-        f.dpost_w = dpost_w;
-        f.dpost_b = dpost_b;
-        f.dpre_w = dpre_w;
-        f.dpre_b = dpre_b;
+    if (params && !alone) {                // (no rows: zeros)
         const dim3 grid(unsigned((p.N + kFinCols - 1) / kFinCols), 2), block(kFinCols * kFinGroups);
         if (full)
             COMERA_LAUNCH((block_norm_finish_kernel<2>), grid, block, 0, st, f);

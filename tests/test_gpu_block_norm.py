@@ -225,6 +225,17 @@ def test_batches(b, n):
     c.check_backward()
 
 
+@pytest.mark.parametrize("post,pre,gate,bias", [("layer", "rms", "channel", True), ("rms", "rms", "channel", False),
+                                                ("rms", "layer", "token", False), ("none", "rms", "none", False)])
+@pytest.mark.parametrize("b,n", [(2, 5), (17, 5), (64, 40), (65, 40), (33, 200), (9, 300), (16, 768), (17, 768),
+                                 (8, 1001), (9, 1001), (5, 2048), (2, 4096), (3, 4096), (1, 4097), (2, 8192)])
+def test_few_rows(b, n, post, pre, gate, bias):
+    """Up to two turns of one workgroup, which forms the parameters' gradients itself, and one row more."""
+    c = Case(b, n, TYPES[b % 3], post, pre, gate, bias=bias)
+    c.check_backward()
+    c.check_backward(leave_out=("dX", "dF", "dpre_w") if gate == "token" else ("dX", "dF", "dpost_w"))
+
+
 def test_large_mean():
     """A mean of 100 spreads: the variance is taken around the mean."""
     c = Case(6, 768, TYPES[0], "layer", "layer", "token", mean=100.0)
