@@ -212,7 +212,8 @@ __global__ __launch_bounds__(kGroupThreads) void dense_count_kernel(GroupArgs a)
 // lower workgroups on the walk, which needs no other launch; with more parts
 // it adds up what dense_count_kernel counted.  Every id is read by G
 // workgroups, from the L2; bound by the instructions of the walk, about 10
-// per 64 ids and wave.
+// per 64 ids and wave, and by its chain of waits: 9.1 us for 16384 ids of 256
+// workgroups.
 __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a) {
     extern __shared__ uint32_t cnt[];                  // [kGroupWaves][Q]
     __shared__ uint32_t wsum[kGroupWaves], wbelow[kGroupWaves], longs;
@@ -569,8 +570,8 @@ __global__ __launch_bounds__(64 * kFinishWaves) void dense_finish_kernel(SumArgs
 
 // ---------------------------------------------------------------- host side
 // From here on one more launch costs less than the walk of all ids by every
-// workgroup: 16384 Zipf ids 44.1 us in one part, 45.5 in four; 32768: 56.9 and
-// 54.3; 131072: 140.7 and 96.3 (table of 32768 x 768)
+// workgroup: 16384 Zipf ids 39.0 us in one part, 40.5 in two launches; 32768:
+// 51.2 and 50.0; 131072: 132 and 92 (table of 32768 x 768)
 constexpr int64_t kSplitTokens = 24576;
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }

@@ -37,7 +37,8 @@ constexpr int kScaleBlocks = 2048;     // workgroups of one launch of the second
 // From here on (bytes read and written) the clipped gradients are stored
 // around the last-level cache: their lines would leave it only during the
 // next pass, and throw out what that pass could still find there.  272 MB:
-// both passes together 110 -> 97 us.
+// both passes together 90.7 -> 76.5 us, with an update behind them that reads
+// the results and a state of their size 155 -> 148.
 constexpr double kStreamBytes = 192.0 * 1048576;
 constexpr int64_t kBf16 = int64_t(1) << 62;
 
