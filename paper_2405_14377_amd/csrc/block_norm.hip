@@ -325,6 +325,18 @@ struct BwdRows {
             if (p.gate) g[j].load(static_cast<const TA *>(p.gate) + at + k.col[j]);
         }
     }
+    __device__ __forceinline__ void arrive(const NormArgs &p) const {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            if (p.dXn) t[j].arrive();
+            if (p.dH) {
+                x[j].arrive();
+                h[j].arrive();
+            }
+            if (p.F) f[j].arrive();
+            if (p.gate) g[j].arrive();
+        }
+    }
     // zeros for the entries that are not the lane's own; a row that is not
     // live adds nothing to any sum
     __device__ __forceinline__ void clear(const NormArgs &p, const Columns<VEC, CH> &k, bool live) {
@@ -357,6 +369,12 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p, Alone..
     // two tokens' rows do not fit the registers with 16 entries a lane, nor with
     // 12 in fp32 and every sum (4096 x 768 LAYER: 27.4 us with spills, 20.0)
     constexpr bool AHEAD = NE <= 8 || (NE <= 12 && !(FULL && sizeof(TS) == 4 && sizeof(TA) == 4));
+    // The loop's end waits for the next token's rows, and with them for stores
+    // behind those loads.  All stores after that wait: 16384 x 4096 155.1 ->
+    // 149.1 us, 32768 x 512 45.6 -> 44.7.  Not in fp32 (8192 x 2048 81.3 ->
+    // 82.0), nor with every sum (8191 x 1001 50.5 -> 51.7) or narrow rows
+    // (65536 x 128 24.6 -> 25.2).
+    constexpr bool LATE = !FULL && VEC == 8 && CH == 1 && LPR == 0 && sizeof(TS) == 2 && sizeof(TA) == 2;
     __shared__ __attribute__((aligned(16))) float red[2][8][4];
     extern __shared__ float share[];       // [2][rows][N] when rows > 1
     int turn = 0;
@@ -447,13 +465,13 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p, Alone..
                 t[i] += r * (FULL ? h * w[i] - su - y * sy : h * w[i] - y * sy);
             }
         }
-        if (p.dX && live) {
-            float o[NE];
+        float dx[NE];
+        {
             const float a = p.F ? p.a : 1.f;
 #pragma unroll
-            for (int i = 0; i < NE; ++i) o[i] = a * t[i];
-            store_row<TS, VEC, CH>(p.dX, at, k, o);
+            for (int i = 0; i < NE; ++i) dx[i] = a * t[i];
         }
+        if ((!LATE || !p.F) && p.dX && live) store_row<TS, VEC, CH>(p.dX, at, k, dx);
         if (!p.F) continue;
         if constexpr (FULL) k.clear(t);
         const float r = p.post != COMERA_NORM_NONE ? rsqrtf(s[3] * inv_n + p.eps) : 1.f;
@@ -468,6 +486,7 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p, Alone..
                 z[i] = p.beta * t[i] * (f[i] * z[i] + o[i]);
                 t[i] *= in.g[i / VEC].get(i % VEC);
             }
+            if constexpr (LATE) next.arrive(p);
             if (p.dgate && live) store_row<TA, VEC, CH>(p.dgate, at, k, z);
         }
         float q[2] = {0.f, 0.f};
@@ -484,6 +503,10 @@ __global__ __launch_bounds__(512) void block_norm_bwd_kernel(NormArgs p, Alone..
             const float sy = q[0] * inv_n, su = post_mean ? q[1] * inv_n : 0.f;
 #pragma unroll
             for (int i = 0; i < NE; ++i) t[i] = r * (FULL ? t[i] - su - f[i] * sy : t[i] - f[i] * sy);
+        }
+        if constexpr (LATE) {
+            next.arrive(p);
+            if (p.dX && live) store_row<TS, VEC, CH>(p.dX, at, k, dx);
         }
         if (p.dF && live) store_row<TA, VEC, CH>(p.dF, at, k, t);
     }

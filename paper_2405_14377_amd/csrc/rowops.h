@@ -116,6 +116,10 @@ struct Pack<bf16, V> {
             x[0] = p->bits;
         }
     }
+    __device__ __forceinline__ void arrive() const {       // waits for the load
+#pragma unroll
+        for (int i = 0; i < (V + 1) / 2; ++i) asm volatile("" ::"v"(x[i]) : "memory");
+    }
     __device__ __forceinline__ float get(int i) const { return i & 1 ? hi_bf16(x[i / 2]) : lo_bf16(x[i / 2]); }
     __device__ __forceinline__ void clear(int first) {     // entries [0, first)
 #pragma unroll
