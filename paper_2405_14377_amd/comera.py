@@ -204,9 +204,10 @@ def _ptr_array(xs: Optional[Sequence]):
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
+        if _torch is None:
+            raise ImportError("the current stream is torch's: pass a stream")
         # the handle alone: building a Stream object costs 3 us a call
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return _torch._C._cuda_getCurrentRawStream(_torch._C._cuda_getDevice())
     if isinstance(stream, int):
         return stream
     return int(stream.cuda_stream)
