@@ -240,6 +240,7 @@ __global__ __launch_bounds__(kGroupThreads) void dense_group_kernel(GroupArgs a)
     uint32_t whole = 0, before = 0;
     if (a.parts > 1) {
         if (t < Q)
+#pragma unroll 8
             for (int x = 0; x < a.parts; ++x) {
                 const uint32_t c = a.count[(int64_t(x) * groups + g) * Q + t];
                 whole += c;
@@ -425,17 +426,20 @@ constexpr int kFewQ = 64;              // most ids of one workgroup: a bit each
 constexpr int kFewLoads = 16;          // rows in flight per wave
 
 // All of a small batch's gradient in one launch.  Workgroup g owns the ids
-// with id mod G = g: it lists its tokens in order, writes zeros for its ids
-// without tokens, a wave per row, and adds the rows of the others, a wave per
-// id and column slice.  Bound by launch latency and the zeros: 300 uniform
-// ids of 2000 x 640 bf16 8.0 us (three launches: 14.5), 1000 Zipf ids of 8000
-// x 768 11.4 us (17.7), 64 ids of 20000 x 768 10.8 us (19.5).
+// with id mod G = g: it lists its tokens in order, adds the rows of its ids
+// that have any, a wave per id and column slice (or several, where tokens are
+// many and pairs few), and writes zeros for the others, a wave per row.
+// Bound by launch latency and the zeros: 300 uniform ids of 2000 x 640 bf16
+// 7.7 us (three launches: 14.5), 1000 Zipf ids of 8000 x 768 10.9 us (17.7),
+// 64 ids of 20000 x 768 10.7 us (19.5); 300 tokens of two ids 9.9 us (with a
+// wave per pair 14.9).
 template <class TY, class TT, int VEC>
 __global__ __launch_bounds__(kFewTokens) void dense_few_kernel(GroupArgs a, SumArgs b) {
     constexpr int kWaves = kFewTokens / 64;
     __shared__ uint2 list[kFewTokens];                 // (token, id)
     __shared__ uint32_t wcount[kWaves];
     __shared__ unsigned long long present;
+    __shared__ float red[kWaves][64 * VEC];
     const int t = threadIdx.x, w = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
     const uint32_t g = blockIdx.x, mask = (1u << a.lg) - 1;
     if (t == 0) present = 0;
@@ -462,42 +466,78 @@ __global__ __launch_bounds__(kFewTokens) void dense_few_kernel(GroupArgs a, SumA
     const int64_t E = b.E;
     const TY *dY = static_cast<const TY *>(b.dY);
     TT *dT = static_cast<TT *>(b.dT);
-    // ids with tokens first: their loads are on their way while zeros are written
-    int job = 0;
-    for (unsigned long long p = all; p; p &= p - 1) {
-        const uint32_t q = uint32_t(__ffsll(p)) - 1;
-        for (int s = 0; s < b.slices; ++s, ++job) {
-            if (job % kWaves != w) continue;
-            const int64_t c0 = int64_t(s) * 64 * VEC + lane * VEC, c = c0 < E ? min(c0, E - VEC) : 0;
-            float acc[VEC];
+    // acc += the rows of id q's tokens at places [i, end) of the list
+    auto add = [&](uint32_t q, uint32_t i, uint32_t end, int64_t c, float (&acc)[VEC]) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-            for (uint32_t i = 0; i < n; i += 64) {
-                const uint2 x = list[min(i + lane, n - 1)];
-                uint64_t todo = __ballot(i + lane < n && (x.y >> a.lg) == q);
-                while (todo) {
-                    Pack<TY, VEC> r[kFewLoads];
-                    int k1 = 0, bit = 0;
+        for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+        for (; i < end; i += 64) {
+            const uint2 x = list[min(i + lane, end - 1)];
+            uint64_t todo = __ballot(i + lane < end && (x.y >> a.lg) == q);
+            while (todo) {
+                Pack<TY, VEC> r[kFewLoads];
+                int k1 = 0, bit = 0;
 #pragma unroll
-                    for (int k = 0; k < kFewLoads; ++k) {
-                        // behind the last token its row is read again
-                        if (todo) {
-                            bit = __ffsll((unsigned long long)todo) - 1;
-                            todo &= todo - 1;
-                            k1 = k + 1;
-                        }
-                        r[k].load(dY + int64_t(uint32_t(__builtin_amdgcn_readlane(int(x.x), bit))) * E + c);
+                for (int k = 0; k < kFewLoads; ++k) {
+                    // behind the last token its row is read again
+                    if (todo) {
+                        bit = __ffsll((unsigned long long)todo) - 1;
+                        todo &= todo - 1;
+                        k1 = k + 1;
                     }
-#pragma unroll
-                    for (int k = 0; k < kFewLoads; ++k)
-                        if (k < k1)
-#pragma unroll
-                            for (int e = 0; e < VEC; ++e) acc[e] += r[k].get(e);
+                    r[k].load(dY + int64_t(uint32_t(__builtin_amdgcn_readlane(int(x.x), bit))) * E + c);
                 }
-            }
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) acc[e] *= b.scale;
-            if (c0 < E) Pack<TT, VEC>::store(dT + ((int64_t(q) << a.lg) + g) * E + c, acc);
+                for (int k = 0; k < kFewLoads; ++k)
+                    if (k < k1)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) acc[e] += r[k].get(e);
+            }
+        }
+    };
+    auto store = [&](uint32_t q, int64_t c, float (&acc)[VEC]) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) acc[e] *= b.scale;
+        Pack<TT, VEC>::store(dT + ((int64_t(q) << a.lg) + g) * E + c, acc);
+    };
+    // ids with tokens first: their loads are on their way while zeros are written
+    const int jobs = __builtin_amdgcn_readfirstlane(min(__popcll(all) * b.slices, kWaves));
+    if (n <= 2 * kFewLoads || jobs > kWaves / 2) {
+        int job = 0;
+        for (unsigned long long p = all; p; p &= p - 1) {
+            const uint32_t q = uint32_t(__ffsll(p)) - 1;
+            for (int s = 0; s < b.slices; ++s, ++job) {
+                if (job % kWaves != w) continue;
+                const int64_t c0 = int64_t(s) * 64 * VEC + lane * VEC, c = c0 < E ? min(c0, E - VEC) : 0;
+                float acc[VEC];
+                add(q, 0, n, c, acc);
+                if (c0 < E) store(q, c, acc);
+            }
+        }
+    } else {
+        // ids and slices for half of the waves at most: several waves a pair,
+        // their sums added in order
+        const int split = min(kWaves / jobs, int(n) / kFewLoads), mine = w / split, part = w % split;
+        uint32_t q = 0;
+        int64_t c0 = E;
+        int job = 0;
+        for (unsigned long long p = all; p; p &= p - 1, job += b.slices)
+            if (mine >= job && mine < job + b.slices) {
+                q = uint32_t(__ffsll(p)) - 1;
+                c0 = int64_t(mine - job) * 64 * VEC + lane * VEC;
+            }
+        const int64_t c = c0 < E ? min(c0, E - VEC) : 0;
+        float acc[VEC];
+        if (mine < jobs) {
+            add(q, n * part / split, n * (part + 1) / split, c, acc);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) red[w][lane * VEC + e] = acc[e];
+        }
+        __syncthreads();
+        if (mine < jobs && part == 0 && c0 < E) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                for (int k = 1; k < split; ++k) acc[e] += red[w + k][lane * VEC + e];
+            store(q, c, acc);
         }
     }
     for (int q = w; q < a.Q; q += kWaves) {
@@ -609,13 +649,18 @@ void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L)
     };
     // 256 workgroups (more where one would own more ids than its LDS counts).
     // A long batch is cut into parts, each id read by fewer workgroups: as
-    // few as own all ids, in as many parts as make 256 of them.
+    // few as own all ids, in as many parts as make 256 of them (32 at most);
+    // so is a shorter one of a few ids, whose tokens few workgroups own: 16384
+    // of 2 ids 41.3 -> 33.4 us, of 16 20.2 -> 22.7, 8192 of 2 26.2 -> 29.9.
     // A batch of one id a thread is done by one launch (with more tables rows
-    // than 2^22 its workgroups would be too many).
-    L.few_tokens = n <= kFewTokens && s->V <= int64_t(kFewQ) << 16;
+    // than 2^22 its workgroups would be too many), unless a few ids leave it
+    // to a few CUs: 1000 tokens of 2 ids 20.2 us, 14.8 by the general way; 300
+    // 10.2 and 14.1.
+    L.few_tokens = n <= std::min<int64_t>(kFewTokens, 256 * s->V) && s->V <= int64_t(kFewQ) << 16;
     L.lg = n < kSplitTokens ? 8 : 5;
     while (((s->V - 1) >> L.lg) >= (L.few_tokens ? kFewQ : kGroupQ)) ++L.lg;
-    L.parts = n < kSplitTokens ? 1 : std::max(1, 256 >> L.lg);
+    const bool split = n >= (s->V > 4 ? kSplitTokens : kSplitTokens / 2);
+    L.parts = split ? int(std::min<int64_t>(32, std::max<int64_t>(1, 256 / std::min(L.groups(), s->V)))) : 1;
     L.Q = int((s->V - 1) >> L.lg) + 1;
     // longer chunks leave fewer partial rows, shorter ones more waves
     L.lgC = n < 32768 ? 4 : 5;
@@ -679,10 +724,19 @@ void launch_sum(const GroupArgs &ga, SumArgs a, const DenseLayout_ &L, hipStream
     a.sum_blocks = uint32_t(std::min(kMost, (a.jobs + 3) / 4));
     const uint32_t fill = uint32_t(std::min(kMost, (a.V + kFillIds - 1) / kFillIds));
     COMERA_LAUNCH((dense_sum_kernel<TY, TT, VEC>), dim3(a.sum_blocks + fill), dim3(256), 0, st, a);
-    COMERA_LAUNCH((dense_finish_kernel<TT, VEC>),
-                  dim3(unsigned(std::min<int64_t>(groups, 1 << 16)), unsigned(std::min(a.slices, 16)),
-                       unsigned(std::max<int64_t>(1, 256 / groups))),
-                  dim3(64 * kFinishWaves), 0, st, a, int(groups));
+    const auto finish = [&](auto kernel) {
+        COMERA_LAUNCH(kernel, dim3(unsigned(std::min<int64_t>(groups, 1 << 16)), unsigned(std::min(a.slices, 16)),
+                                   unsigned(std::max<int64_t>(1, 256 / groups))),
+                      dim3(64 * kFinishWaves), 0, st, a, int(groups));
+    };
+    // a table of a few rows: narrower slices, more workgroups (131072 tokens
+    // of one id 168 -> 113 us, of 16 ids 66 -> 60, with the parts above)
+    if (a.V * a.slices >= 64) {
+        finish(dense_finish_kernel<TT, VEC>);
+    } else {
+        a.slices = int((a.E + 63) / 64);
+        finish(dense_finish_kernel<TT, 1>);
+    }
 }
 
 template <class TY, class TT>

@@ -95,6 +95,20 @@ def test_backward_sizes(V, E, n, kind):
     _check_backward(got.np(), V, ids, dY, 0.5, -1, "f32")
 
 
+# one launch up to 256 tokens a row, its waves shared by one id; parts from 12288 tokens
+@pytest.mark.parametrize("kind", ["uniform", "hot", "same"])
+@pytest.mark.parametrize("V,E,n", [(1, 100, 17), (1, 768, 256), (1, 768, 257), (1, 3, 1024), (2, 768, 512),
+                                   (2, 1001, 513), (3, 260, 700), (6, 2100, 1000), (5000, 768, 900), (1, 260, 12287),
+                                   (1, 260, 12288), (4, 33, 12288), (2, 515, 16384), (2, 1, 16384), (3, 64, 40001), (17, 768, 2500)])
+def test_backward_few_rows(V, E, n, kind):
+    rng = np.random.default_rng(n + E)
+    act = ("f32", "bf16")[n % 2]
+    ids, dY = _ids(rng, n, V, kind), values(rng.standard_normal((n, E)), act)
+    pad = (-1, V - 1)[E % 2]
+    got = _backward(V, E, ids, dY, 0.5, pad, act=act, offset=n % 3)
+    _check_backward(got.np(), V, ids, dY, 0.5, pad, "f32")
+
+
 @pytest.mark.parametrize("table", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["f32", "bf16"])
 @pytest.mark.parametrize("V,E,n,offset", [(90, 768, 400, 0), (90, 1001, 400, 1), (40, 7, 200, 3), (31, 520, 3000, 0),
