@@ -99,7 +99,8 @@ def test_backward_sizes(V, E, n, kind):
 @pytest.mark.parametrize("kind", ["uniform", "hot", "same"])
 @pytest.mark.parametrize("V,E,n", [(1, 100, 17), (1, 768, 256), (1, 768, 257), (1, 3, 1024), (2, 768, 512),
                                    (2, 1001, 513), (3, 260, 700), (6, 2100, 1000), (5000, 768, 900), (1, 260, 12287),
-                                   (1, 260, 12288), (4, 33, 12288), (2, 515, 16384), (2, 1, 16384), (3, 64, 40001), (17, 768, 2500)])
+                                   (1, 260, 12288), (4, 33, 12288), (2, 515, 16384), (2, 1, 16384), (3, 64, 40001),
+                                   (17, 768, 2500)])
 def test_backward_few_rows(V, E, n, kind):
     rng = np.random.default_rng(n + E)
     act = ("f32", "bf16")[n % 2]
