@@ -358,8 +358,8 @@ typedef struct {
     int32_t act;                          /* comera_dtype of Y, dY */
 } comera_dense_embed_shape;
 
-/* Workspace bytes of comera_dense_embed_backward (0 for a shape or a number
- * of tokens that is refused). */
+/* Workspace bytes of comera_dense_embed_backward for any batch of up to
+ * n_tokens (0 for a shape or a number of tokens that is refused). */
 size_t comera_dense_embed_workspace_bytes(const comera_dense_embed_shape *s, int64_t n_tokens);
 
 /* Y[t, :] = scale * T[ids[t], :] for t < n_tokens, formed in fp32 and
@@ -410,8 +410,8 @@ typedef struct {
     float res_scale, branch_scale;
 } comera_block_norm_shape;
 
-/* Workspace bytes of comera_block_norm_backward for b rows (0 for a shape
- * that is refused). */
+/* Workspace bytes of comera_block_norm_backward for any batch of up to b rows
+ * (0 for a shape that is refused). */
 size_t comera_block_norm_workspace_bytes(const comera_block_norm_shape *s, int64_t b);
 
 /* Xn [b, width] and H [b, width] from X and F [b, width], rows contiguous;

@@ -613,6 +613,8 @@ __global__ __launch_bounds__(64 * kFinishWaves) void dense_finish_kernel(SumArgs
 // workgroup: 16384 Zipf ids 39.0 us in one part, 40.5 in two launches; 32768:
 // 51.2 and 50.0; 131072: 132 and 92 (table of 32768 x 768)
 constexpr int64_t kSplitTokens = 24576;
+// From here on chunks of 32 places instead of 16
+constexpr int64_t kLongChunks = 32768;
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -640,6 +642,9 @@ bool dense_backward_supported(const comera_dense_embed_shape *s) {
     return dense_supported(s) && s->V <= int64_t(kGroupQ) << 21;
 }
 
+// the longest batch that one launch does, where the table is not too long for it
+int64_t most_few_tokens(const comera_dense_embed_shape *s) { return std::min<int64_t>(kFewTokens, 256 * s->V); }
+
 void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L) {
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -656,14 +661,14 @@ void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L)
     // than 2^22 its workgroups would be too many), unless a few ids leave it
     // to a few CUs: 1000 tokens of 2 ids 20.2 us, 14.8 by the general way; 300
     // 10.2 and 14.1.
-    L.few_tokens = n <= std::min<int64_t>(kFewTokens, 256 * s->V) && s->V <= int64_t(kFewQ) << 16;
+    L.few_tokens = n <= most_few_tokens(s) && s->V <= int64_t(kFewQ) << 16;
     L.lg = n < kSplitTokens ? 8 : 5;
     while (((s->V - 1) >> L.lg) >= (L.few_tokens ? kFewQ : kGroupQ)) ++L.lg;
     const bool split = n >= (s->V > 4 ? kSplitTokens : kSplitTokens / 2);
     L.parts = split ? int(std::min<int64_t>(32, std::max<int64_t>(1, 256 / std::min(L.groups(), s->V)))) : 1;
     L.Q = int((s->V - 1) >> L.lg) + 1;
     // longer chunks leave fewer partial rows, shorter ones more waves
-    L.lgC = n < 32768 ? 4 : 5;
+    L.lgC = n < kLongChunks ? 4 : 5;
     // an id that begins at a chunk's last place ends within the 64 lanes
     L.few = std::min(64 - (1 << L.lgC), 1 << L.lgC);
     L.chunks = (n + (1 << L.lgC) - 1) >> L.lgC;
@@ -680,6 +685,20 @@ void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L)
     L.first = take(sizeof(float) * size_t(L.chunks) * size_t(s->E));
     L.last = take(sizeof(float) * size_t(L.chunks) * size_t(s->E));
     L.bytes = off;
+}
+
+// The most that any batch of up to n tokens needs, so that the workspace of a
+// program's longest batch serves its shorter ones.  What a batch needs grows
+// with it except where dense_layout changes its form, which may halve it.
+size_t dense_most_bytes(const comera_dense_embed_shape *s, int64_t n) {
+    size_t most = 0;
+    for (const int64_t last : {most_few_tokens(s), kSplitTokens / 2 - 1, kSplitTokens - 1, kLongChunks - 1, n}) {
+        if (last > n) continue;
+        DenseLayout_ L{};
+        dense_layout(s, last, L);
+        most = std::max(most, L.bytes);
+    }
+    return most;
 }
 
 comera_status dense_status() { return note_hip(launch_status(), "dense embedding") ? COMERA_ERR_HIP : COMERA_OK; }
@@ -756,9 +775,7 @@ extern "C" {
 
 size_t comera_dense_embed_workspace_bytes(const comera_dense_embed_shape *s, int64_t n_tokens) {
     if (!dense_ok(s) || !dense_backward_supported(s) || n_tokens < 0 || n_tokens >= 2147483647) return 0;
-    DenseLayout_ L{};
-    dense_layout(s, n_tokens, L);
-    return L.bytes;
+    return dense_most_bytes(s, n_tokens);
 }
 
 comera_status comera_dense_embed_forward(const comera_dense_embed_shape *s, const int64_t *ids, int64_t n_tokens,

@@ -1,0 +1,40 @@
+"""What the calls around the layers promise beyond one call: workspaces of a
+longest batch, a long list's table, raw addresses (no GPU: launch check mode,
+placeholder addresses)."""
+import pytest
+
+from paper_2405_14377_amd import comera as C
+
+FAKE = 1 << 40
+
+
+@pytest.fixture
+def checked():
+    C.comera_debug_launch_check(True)
+    yield
+    C.comera_debug_launch_check(False)
+
+
+# token counts around every change of the table gradient's form, for tables of more than four rows and of fewer
+COUNTS = (0, 1, 100, 255, 256, 257, 511, 512, 513, 1023, 1024, 1025, 2000, 12287, 12288, 12289, 24575, 24576, 24577,
+          32767, 32768, 32769, 60000, 131072)
+
+
+@pytest.mark.parametrize("V,E", [(1, 8), (2, 64), (4, 16), (5, 3), (100, 8), (2000, 640), (32768, 768), (70000, 4),
+                                 (600000, 1), (4194304, 2), (4194305, 2)])
+def test_embed_workspace_of_the_longest_batch(checked, V, E):
+    """A workspace for n tokens serves every batch of up to n."""
+    lib = C.load()
+    s = C.dense_embed_shape(V, E, C.F32, C.BF16)
+    sizes = [C.comera_dense_embed_workspace_bytes(s, n) for n in COUNTS]
+    assert sizes == sorted(sizes)
+    for i, most in enumerate(sizes):
+        for n in COUNTS[:i + 1]:
+            assert lib.comera_dense_embed_backward(s, FAKE, n, FAKE, 1.0, -1, FAKE, FAKE, most, None, 0) == C.OK, n
+
+
+@pytest.mark.parametrize("width", [1, 8, 128, 256, 768, 1000, 4096, 5000, 8192])
+def test_norm_workspace_of_the_longest_batch(width):
+    s = C.block_norm_shape(width, pre=C.NORM_LAYER)
+    sizes = [C.comera_block_norm_workspace_bytes(s, b) for b in range(3000)]
+    assert sizes == sorted(sizes)
