@@ -281,6 +281,8 @@ struct comera_grad_plan_s {
     int parts = 0;
     bool stream = false;                   // more bytes than the last-level cache holds
     comera::GradTable table{};             // e: null without one
+    bool written = false;                  // not where launch check mode only recorded the table's launches
+    bool has_table() const { return table.e && (written || comera::launch_check_mode()); }
 };
 
 using namespace comera;
@@ -302,7 +304,7 @@ comera_status grad_args(comera_grad_plan_t p, float scale, const void *ws, size_
 
 // the first pass; returns the number of partials
 int launch_squares(comera_grad_plan_t p, double *part, hipStream_t st) {
-    if (p->table.e) {
+    if (p->has_table()) {
         COMERA_LAUNCH((grad_squares_kernel<GradTable>), dim3(unsigned(p->table.parts)), dim3(kGradThreads), 0, st,
                       p->table, part);
         return p->table.parts;
@@ -418,6 +420,7 @@ comera_status comera_grad_plan_set_table(comera_grad_plan_t p, void *table, size
     }
     if (note_hip(launch_status(), "gradient table")) return COMERA_ERR_HIP;
     p->table.e = static_cast<const Entry *>(table);
+    p->written = !launch_check_mode();
     return COMERA_OK;
 }
 
@@ -452,7 +455,7 @@ comera_status comera_grad_clip(comera_grad_plan_t p, float scale, float max_norm
         return note_hip(launch_status(), "gradient clipping") ? COMERA_ERR_HIP : COMERA_OK;
     }
     launch_squares(p, part, st);
-    if (p->table.e)
+    if (p->has_table())
         launch_scale(p, p->table, part, scale, max_norm, norm, flag, st);
     else
         for (size_t i = p->chunks.size(); i-- > 0;)    // last read, first scaled

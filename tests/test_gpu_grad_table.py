@@ -1,0 +1,67 @@
+"""A long list's table of gradient tensors on the GPU: which table a call
+reads, and for how long.
+
+Every buffer here that a call could take for a table holds a whole one, of
+other outputs, so a call that reads the wrong one writes those outputs.
+Tolerance of a clipped entry: one fp32 product with a factor that is itself
+rounded once.
+"""
+import pytest
+
+from paper_2405_14377_amd import comera as C
+from tests.step_util import U
+
+pytestmark = pytest.mark.gpu
+
+COUNT = 130                          # more than one launch's arguments hold
+
+
+class List:
+    """Gradients (given or new), their outputs and a plan of them."""
+
+    def __init__(self, grads=None):
+        import torch
+        self.g = grads or [torch.randn(5 + 7 * i % 40, device="cuda") for i in range(COUNT)]
+        self.out = [torch.full_like(x, float("nan")) for x in self.g]
+        self.plan = C.GradPlan(self.g, self.out)
+        assert self.plan.table is not None
+        self.ws = torch.empty(self.plan.workspace_bytes, dtype=torch.uint8, device="cuda")
+        self.norm = torch.full((1,), float("nan"), device="cuda")
+
+    def clip(self, **k):
+        C.comera_grad_clip(self.plan.handle, 1.0, 0.5, self.norm, None, self.ws, **k)
+
+    def check(self):
+        import torch
+        want = sum(float(x.double().square().sum()) for x in self.g) ** 0.5
+        assert self.norm.item() == pytest.approx(want, rel=2 * U)
+        for x, y in zip(self.g, self.out):
+            assert torch.allclose(y.double(), x.double() * (0.5 / want), rtol=4 * U, atol=0)
+
+    def untouched(self):
+        return all(x.isnan().all() for x in self.out) and self.norm.isnan().all()
+
+
+def test_table_set_in_check_mode_is_not_read():
+    """Launch check mode writes no table: a call outside it goes without."""
+    import torch
+    torch.manual_seed(1)
+    a = List()
+    b = List(a.g)
+    before = a.plan.table.clone()
+    C.comera_debug_launch_check(True)
+    try:
+        C.comera_grad_plan_set_table(b.plan.handle, a.plan.table)
+        b.clip()
+    finally:
+        C.comera_debug_launch_check(False)
+    torch.cuda.synchronize()
+    assert torch.equal(a.plan.table, before) and a.untouched() and b.untouched()
+    b.clip()
+    b.check()
+    assert a.untouched()
+    C.comera_grad_plan_set_table(b.plan.handle, b.plan.table)
+    for x in b.out:
+        x.fill_(float("nan"))
+    b.clip()
+    b.check()
