@@ -411,6 +411,16 @@ comera_status comera_grad_plan_set_table(comera_grad_plan_t p, void *table, size
     const size_t need = comera_grad_table_bytes(p);
     if (!table || need == 0) return COMERA_OK;
     if (bytes < need || reinterpret_cast<uintptr_t>(table) % 8) return COMERA_ERR_WORKSPACE;
+    // a captured table would be written by replays alone, and calls before
+    // the first one would read it
+    if (!launch_check_mode()) {
+        hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+        if (note_hip(int(hipStreamIsCapturing(hipStream_t(stream), &capture)), "gradient table")) {
+            (void)hipGetLastError();       // noted: not the next call's
+            return COMERA_ERR_HIP;
+        }
+        if (capture != hipStreamCaptureStatusNone) return COMERA_ERR_INVALID_ARG;
+    }
     Entry *e = static_cast<Entry *>(table);
     uint32_t tiles = 0;
     for (const GradChunk &c : p->chunks) {

@@ -65,3 +65,37 @@ def test_table_set_in_check_mode_is_not_read():
         x.fill_(float("nan"))
     b.clip()
     b.check()
+
+
+def test_table_set_in_a_capture_is_refused():
+    """A captured table would be written by replays alone: refused, the capture goes on, and the plan is without one."""
+    import torch
+    torch.manual_seed(2)
+    a = List()
+    b = List(a.g)
+    x = torch.ones(3, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        x.add_(1.0)
+        with pytest.raises(C.ComeraError) as e:
+            C.comera_grad_plan_set_table(b.plan.handle, a.plan.table)
+        with pytest.raises(C.ComeraError):
+            C.GradPlan(a.g, a.out)
+        b.clip()
+    assert e.value.status == C.ERR_INVALID_ARG
+    for _ in range(3):
+        for y in b.out + [b.norm]:
+            y.fill_(float("nan"))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        b.check()
+        assert a.untouched()
+    assert (x == 4).all()
+    b.clip()
+    b.check()
+    C.comera_grad_plan_set_table(b.plan.handle, None)          # nothing to write: allowed anywhere
+    a.clip()
+    a.check()
+    del g
