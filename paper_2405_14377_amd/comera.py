@@ -563,11 +563,25 @@ def comera_grad_workspace_bytes(plan) -> int:
     return int(load().comera_grad_workspace_bytes(plan))
 
 
+# GradPlan's tables in device memory: plan handle -> (table, handles of the streams that its memory waits for)
+_tables: dict = {}
+
+
+def _keep_table(plan, stream: int) -> int:
+    """Before a call on `stream`: the table's memory, once released, is given
+    to nobody else until the work on that stream is done.  Returns the stream."""
+    held = _tables.get(plan)
+    if held is not None and stream not in held[1]:
+        held[0].record_stream(_torch.cuda.ExternalStream(stream) if stream else _torch.cuda.default_stream())
+        held[1].add(stream)
+    return stream
+
+
 def comera_grad_norm(plan, scale: float, norm, flag, ws, stream=None) -> int:
     """norm = scale * sqrt(sum of all squares); flag = 1 if it is not finite."""
     lib = load()
     p = _taken("comera_grad_norm", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
-    st = lib.comera_grad_norm(plan, float(scale), *p, _nbytes(ws), _stream(stream))
+    st = lib.comera_grad_norm(plan, float(scale), *p, _nbytes(ws), _keep_table(plan, _stream(stream)))
     _check(st, "comera_grad_norm")
     return st
 
@@ -576,7 +590,8 @@ def comera_grad_clip(plan, scale: float, max_norm: float, norm, flag, ws, stream
     """The norm, and out = scale * min(1, max_norm / norm) * g for every tensor of the plan."""
     lib = load()
     p = _taken("comera_grad_clip", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
-    st = lib.comera_grad_clip(plan, float(scale), float(max_norm), *p, _nbytes(ws), _stream(stream))
+    st = lib.comera_grad_clip(plan, float(scale), float(max_norm), *p, _nbytes(ws),
+                              _keep_table(plan, _stream(stream)))
     _check(st, "comera_grad_clip")
     return st
 
@@ -585,7 +600,14 @@ class GradPlan:
     """Owns the plan of a list of gradient tensors and a long list's table,
     and keeps the tensors alive.  outs: where the clipped gradients go (None,
     or a None entry: in place).  Made outside a graph capture: a table is
-    waited for, so that calls on any stream find it."""
+    waited for, so that calls on any stream find it.
+
+    The plan may be dropped while calls through this module are pending: its
+    table is kept until they are done (streams of one's own have to exist until
+    the plan is dropped).  A captured graph holds the table's address: keep the
+    plan as long as the graph is replayed.  The gradients and outs are the
+    caller's tensors, whose use on other streams than their own is the caller's
+    to record, as for every call here."""
 
     def __init__(self, grads, outs=None):
         self.handle = None
@@ -612,6 +634,7 @@ class GradPlan:
             self.table = _torch.empty(nbytes, dtype=_torch.uint8, device=self.grads[0].device)
             comera_grad_plan_set_table(self.handle, self.table)
             _torch.cuda.current_stream().synchronize()
+            _tables[self.handle] = self.table, {_stream(None)}     # whose memory it is
 
     @property
     def workspace_bytes(self) -> int:
@@ -619,6 +642,7 @@ class GradPlan:
 
     def __del__(self):
         try:
+            _tables.pop(self.handle, None)
             comera_grad_plan_destroy(self.handle)
         except Exception:
             pass

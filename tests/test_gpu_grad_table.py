@@ -99,3 +99,32 @@ def test_table_set_in_a_capture_is_refused():
     a.clip()
     a.check()
     del g
+
+
+def test_plan_dropped_while_a_call_is_pending():
+    """The table's memory is not given away before a call on another stream has read it."""
+    import torch
+    torch.manual_seed(3)
+    a = List()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+        a.clip()
+    at, size = a.plan.table.data_ptr(), a.plan.table.numel()
+    a.plan = None
+    new = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    pending = not side.query()
+    assert pending and at not in [x.data_ptr() for x in new]
+    for x in new:
+        x.fill_(0)
+    side.synchronize()
+    a.check()
+    # and on a stream of its caller's, given by its handle; on the default one, by 0
+    for stream in (side.cuda_stream, 0):
+        b = List(a.g)
+        torch.cuda.synchronize()
+        b.clip(stream=stream)
+        b.plan = None
+        torch.cuda.synchronize()
+        b.check()

@@ -38,3 +38,54 @@ def test_norm_workspace_of_the_longest_batch(width):
     s = C.block_norm_shape(width, pre=C.NORM_LAYER)
     sizes = [C.comera_block_norm_workspace_bytes(s, b) for b in range(3000)]
     assert sizes == sorted(sizes)
+
+
+class OnDevice:
+    """Host tensors that say they are on device 0, streams by their handles, and what a table was recorded on."""
+
+    def __init__(self, monkeypatch, current=7):
+        import torch
+        self.recorded = []
+        outer = self
+
+        class Tensor(torch.Tensor):
+            def get_device(self):
+                return 0
+
+            def record_stream(self, stream):
+                outer.recorded.append(stream)
+
+        class Current:
+            cuda_stream = current
+
+            def synchronize(self):
+                pass
+
+        empty = torch.empty
+        self.tensor = lambda *a, **k: empty(*a, **{**k, "device": "cpu"}).as_subclass(Tensor)
+        monkeypatch.setattr(torch, "empty", self.tensor)
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Current())
+        monkeypatch.setattr(torch.cuda, "default_stream", lambda *a: "default")
+        monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, *a: handle)
+        monkeypatch.setattr(C, "_stream", lambda s: current if s is None else s)
+
+
+def test_a_plans_table_is_recorded_on_every_stream(checked, monkeypatch):
+    """A dropped plan's table waits for calls on other streams than the one it was made on."""
+    d = OnDevice(monkeypatch)
+    for count, table in ((120, False), (121, True)):
+        plan = C.GradPlan([d.tensor(4) for _ in range(count)])
+        assert (plan.table is not None) == table
+        ws = d.tensor(plan.workspace_bytes // 4)
+        norm = d.tensor(1)
+        C.comera_grad_clip(plan.handle, 1.0, 1.0, norm, None, ws)             # the stream that made it
+        C.comera_grad_clip(plan.handle, 1.0, 1.0, norm, None, ws, stream=21)
+        C.comera_grad_clip(plan.handle, 1.0, 1.0, norm, None, ws, stream=21)
+        C.comera_grad_norm(plan.handle, 1.0, norm, None, ws, stream=0)
+        C.comera_grad_norm(plan.handle, 1.0, norm, None, ws, stream=22)
+        assert d.recorded == ([21, "default", 22] if table else [])
+        handle = plan.handle
+        assert (handle in C._tables) == table
+        del plan
+        assert handle not in C._tables
