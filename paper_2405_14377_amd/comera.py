@@ -76,12 +76,13 @@ class comera_grad_tensor(ctypes.Structure):
 
 
 _lib = None
-_torch = None          # torch, once load() has imported it
+_torch = None          # torch, once load() has imported it (it may be missing: no tensors then, only addresses)
+_f32 = _bf16 = _i32 = _i64 = None      # its types
 
 
 def load(path: str = LIB_PATH) -> ctypes.CDLL:
     """Load the library once; raise if it has not been built."""
-    global _lib, _torch
+    global _lib, _torch, _f32, _bf16, _i32, _i64
     if _lib is not None:
         return _lib
     if not os.path.exists(path):
@@ -94,6 +95,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     try:
         import torch
         _torch = torch
+        _f32, _bf16, _i32, _i64 = torch.float32, torch.bfloat16, torch.int32, torch.int64
     except ImportError:
         pass
     lib = ctypes.CDLL(path)
@@ -264,7 +266,7 @@ def block_norm_shape(width: int, stream: int = F32, act: int = F32, post: int = 
 # strided view, one that is too short or lies on another device than the
 # current one would be read wrongly or out of its bounds.
 def _dtype_of(code: int):
-    return _torch.bfloat16 if code == BF16 else _torch.float32
+    return _bf16 if code == BF16 else _f32
 
 
 def _taken(where: str, *args) -> list:
@@ -473,8 +475,8 @@ def comera_dense_embed_forward(shape, ids, n_tokens: int, T, scale: float, Y, er
     """Y[t, :] = scale * T[ids[t], :]."""
     lib = load()
     where = "comera_dense_embed_forward"
-    ids, T, Y, err_flag = _taken(where, (ids, _torch.int64, n_tokens), (T, _dtype_of(shape.table), shape.V * shape.E),
-                                 (Y, _dtype_of(shape.act), n_tokens * shape.E), (err_flag, _torch.int32, 1))
+    ids, T, Y, err_flag = _taken(where, (ids, _i64, n_tokens), (T, _dtype_of(shape.table), shape.V * shape.E),
+                                 (Y, _dtype_of(shape.act), n_tokens * shape.E), (err_flag, _i32, 1))
     st = lib.comera_dense_embed_forward(shape, ids, int(n_tokens), T, float(scale), Y, err_flag, _stream(stream))
     _check(st, where)
     return st
@@ -486,10 +488,10 @@ def comera_dense_embed_backward(shape, ids, n_tokens: int, dY, scale: float, pad
     lib = load()
     where = "comera_dense_embed_backward"
     nbytes = _nbytes(ws)
-    ids, dY, dT, ws, err_flag = _taken(where, (ids, _torch.int64, n_tokens),
+    ids, dY, dT, ws, err_flag = _taken(where, (ids, _i64, n_tokens),
                                        (dY, _dtype_of(shape.act), n_tokens * shape.E),
                                        (dT, _dtype_of(shape.table), shape.V * shape.E), (ws, None, 0),
-                                       (err_flag, _torch.int32, 1))
+                                       (err_flag, _i32, 1))
     st = lib.comera_dense_embed_backward(shape, ids, int(n_tokens), dY, float(scale), int(pad_id), dT, ws, nbytes,
                                          err_flag, _stream(stream))
     _check(st, where)
@@ -504,7 +506,7 @@ def comera_block_norm_forward(shape, b: int, X, F, post_w, post_b, gate, pre_w, 
     """Xn = res_scale X + branch_scale gate Npost(F), H = Npre(Xn)."""
     lib = load()
     where = "comera_block_norm_forward"
-    w, f32 = shape.width, _torch.float32
+    w, f32 = shape.width, _f32
     st, act, e = _dtype_of(shape.stream), _dtype_of(shape.act), b * w
     p = _taken(where, (X, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w),
                (gate, act, e) if shape.gate == GATE_TOKEN else (gate, f32, w), (pre_w, f32, w), (pre_b, f32, w),
@@ -519,7 +521,7 @@ def comera_block_norm_backward(shape, b: int, Xn, F, post_w, post_b, gate, pre_w
     """Gradients of comera_block_norm_forward; None for an output that is not wanted."""
     lib = load()
     where = "comera_block_norm_backward"
-    w, f32 = shape.width, _torch.float32
+    w, f32 = shape.width, _f32
     st, act, e = _dtype_of(shape.stream), _dtype_of(shape.act), b * w
     gk = (act, e) if shape.gate == GATE_TOKEN else (f32, w)
     p = _taken(where, (Xn, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w), (gate,) + gk, (pre_w, f32, w),
@@ -580,7 +582,7 @@ def _keep_table(plan, stream: int) -> int:
 def comera_grad_norm(plan, scale: float, norm, flag, ws, stream=None) -> int:
     """norm = scale * sqrt(sum of all squares); flag = 1 if it is not finite."""
     lib = load()
-    p = _taken("comera_grad_norm", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
+    p = _taken("comera_grad_norm", (norm, _f32, 1), (flag, _i32, 1), (ws, None, 0))
     st = lib.comera_grad_norm(plan, float(scale), *p, _nbytes(ws), _keep_table(plan, _stream(stream)))
     _check(st, "comera_grad_norm")
     return st
@@ -589,7 +591,7 @@ def comera_grad_norm(plan, scale: float, norm, flag, ws, stream=None) -> int:
 def comera_grad_clip(plan, scale: float, max_norm: float, norm, flag, ws, stream=None) -> int:
     """The norm, and out = scale * min(1, max_norm / norm) * g for every tensor of the plan."""
     lib = load()
-    p = _taken("comera_grad_clip", (norm, _torch.float32, 1), (flag, _torch.int32, 1), (ws, None, 0))
+    p = _taken("comera_grad_clip", (norm, _f32, 1), (flag, _i32, 1), (ws, None, 0))
     st = lib.comera_grad_clip(plan, float(scale), float(max_norm), *p, _nbytes(ws),
                               _keep_table(plan, _stream(stream)))
     _check(st, "comera_grad_clip")
@@ -616,7 +618,7 @@ class GradPlan:
         if len(self.outs) != len(self.grads):
             raise ComeraError(ERR_INVALID_ARG, "GradPlan: as many outs as grads are expected")
         load()
-        codes = {_torch.float32: F32, _torch.bfloat16: BF16}
+        codes = {_f32: F32, _bf16: BF16}
         rows = []
         for g, o in zip(self.grads, self.outs):
             code, n = codes.get(g.dtype), g.numel()

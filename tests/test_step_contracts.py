@@ -89,3 +89,40 @@ def test_a_plans_table_is_recorded_on_every_stream(checked, monkeypatch):
         assert (handle in C._tables) == table
         del plan
         assert handle not in C._tables
+
+
+WITHOUT_TORCH = """
+import sys
+sys.modules["torch"] = None               # an import of it fails
+from paper_2405_14377_amd import comera as C
+C.comera_debug_launch_check(True)
+at = [(1 << 40) + (i << 36) for i in range(20)]
+s = C.dense_embed_shape(100, 8, C.F32, C.BF16)
+C.comera_dense_embed_forward(s, at[0], 4, at[1], 1.0, at[2], at[3], stream=0)
+n = C.block_norm_shape(64, C.F32, C.BF16, C.NORM_LAYER, C.NORM_LAYER, C.GATE_TOKEN)
+C.comera_block_norm_forward(n, 4, *at[:9], stream=0)
+C.comera_block_norm_backward(n, 4, *at[:11], None, None, None, None, None, stream=0)
+try:
+    C.comera_dense_embed_forward(s, at[0], 4, at[1], 1.0, at[2])
+except ImportError as e:
+    assert "pass a stream" in str(e)
+else:
+    raise AssertionError("a current stream without torch")
+plan = C.GradPlan([])
+assert plan.table is None
+p = C.comera_grad_plan((C.comera_grad_tensor * 1)((at[0], None, 100, C.BF16, 0)), 1)
+"""
+
+
+def _without_torch(code):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr
+
+
+def test_addresses_without_torch():
+    """Raw addresses and a stream need no torch."""
+    _without_torch(WITHOUT_TORCH)
