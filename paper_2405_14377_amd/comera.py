@@ -262,7 +262,8 @@ def block_norm_shape(width: int, stream: int = F32, act: int = F32, post: int = 
 
 # ------------------------------------------------------------------ tensor checks
 # The calls around the compressed layers check the tensors that they are
-# given (raw addresses are taken as they are): a tensor of another type, a
+# given (raw addresses are taken as they are, a workspace's or a table's with
+# its bytes behind it: (address, bytes)): a tensor of another type, a
 # strided view, one that is too short or lies on another device than the
 # current one would be read wrongly or out of its bounds.
 def _dtype_of(code: int):
@@ -291,6 +292,15 @@ def _taken(where: str, *args) -> list:
             raise ComeraError(ERR_INVALID_ARG, f"{where}: {t.numel()} entries where {n} are expected")
         out.append(t.data_ptr())
     return out
+
+
+def _workspace(where: str, ws):
+    """(what _taken checks, bytes) of a workspace or a table: a tensor, an (address, bytes) pair or None."""
+    if ws.__class__ is tuple:
+        return ws[0], int(ws[1])
+    if ws.__class__ is int:
+        raise ComeraError(ERR_WORKSPACE, f"{where}: a workspace at a raw address is given as (address, bytes)")
+    return ws, _nbytes(ws)
 
 
 # ------------------------------------------------------------------ entry points
@@ -487,7 +497,7 @@ def comera_dense_embed_backward(shape, ids, n_tokens: int, dY, scale: float, pad
     """dT[v, :] = scale * the sum of dY's rows of the tokens v; pad_id = -1 for none."""
     lib = load()
     where = "comera_dense_embed_backward"
-    nbytes = _nbytes(ws)
+    ws, nbytes = _workspace(where, ws)
     ids, dY, dT, ws, err_flag = _taken(where, (ids, _i64, n_tokens),
                                        (dY, _dtype_of(shape.act), n_tokens * shape.E),
                                        (dT, _dtype_of(shape.table), shape.V * shape.E), (ws, None, 0),
@@ -524,10 +534,11 @@ def comera_block_norm_backward(shape, b: int, Xn, F, post_w, post_b, gate, pre_w
     w, f32 = shape.width, _f32
     st, act, e = _dtype_of(shape.stream), _dtype_of(shape.act), b * w
     gk = (act, e) if shape.gate == GATE_TOKEN else (f32, w)
+    ws, nbytes = _workspace(where, ws)
     p = _taken(where, (Xn, st, e), (F, act, e), (post_w, f32, w), (post_b, f32, w), (gate,) + gk, (pre_w, f32, w),
                (dXn, st, e), (dH, act, e), (dX, st, e), (dF, act, e), (dgate,) + gk, (dpost_w, f32, w),
                (dpost_b, f32, w), (dpre_w, f32, w), (dpre_b, f32, w), (ws, None, 0))
-    rc = lib.comera_block_norm_backward(shape, int(b), *p, _nbytes(ws), _stream(stream))
+    rc = lib.comera_block_norm_backward(shape, int(b), *p, nbytes, _stream(stream))
     _check(rc, where)
     return rc
 
@@ -555,9 +566,10 @@ def comera_grad_table_bytes(plan) -> int:
 def comera_grad_plan_set_table(plan, table, stream=None) -> int:
     """Write a long list's table to `table` (None: work without one); later calls have to be ordered behind it."""
     lib = load()
-    p = _taken("comera_grad_plan_set_table", (table, None, 0))
-    st = lib.comera_grad_plan_set_table(plan, *p, _nbytes(table), _stream(stream))
-    _check(st, "comera_grad_plan_set_table")
+    where = "comera_grad_plan_set_table"
+    table, nbytes = _workspace(where, table)
+    st = lib.comera_grad_plan_set_table(plan, *_taken(where, (table, None, 0)), nbytes, _stream(stream))
+    _check(st, where)
     return st
 
 
@@ -582,19 +594,22 @@ def _keep_table(plan, stream: int) -> int:
 def comera_grad_norm(plan, scale: float, norm, flag, ws, stream=None) -> int:
     """norm = scale * sqrt(sum of all squares); flag = 1 if it is not finite."""
     lib = load()
-    p = _taken("comera_grad_norm", (norm, _f32, 1), (flag, _i32, 1), (ws, None, 0))
-    st = lib.comera_grad_norm(plan, float(scale), *p, _nbytes(ws), _keep_table(plan, _stream(stream)))
-    _check(st, "comera_grad_norm")
+    where = "comera_grad_norm"
+    ws, nbytes = _workspace(where, ws)
+    p = _taken(where, (norm, _f32, 1), (flag, _i32, 1), (ws, None, 0))
+    st = lib.comera_grad_norm(plan, float(scale), *p, nbytes, _keep_table(plan, _stream(stream)))
+    _check(st, where)
     return st
 
 
 def comera_grad_clip(plan, scale: float, max_norm: float, norm, flag, ws, stream=None) -> int:
     """The norm, and out = scale * min(1, max_norm / norm) * g for every tensor of the plan."""
     lib = load()
-    p = _taken("comera_grad_clip", (norm, _f32, 1), (flag, _i32, 1), (ws, None, 0))
-    st = lib.comera_grad_clip(plan, float(scale), float(max_norm), *p, _nbytes(ws),
-                              _keep_table(plan, _stream(stream)))
-    _check(st, "comera_grad_clip")
+    where = "comera_grad_clip"
+    ws, nbytes = _workspace(where, ws)
+    p = _taken(where, (norm, _f32, 1), (flag, _i32, 1), (ws, None, 0))
+    st = lib.comera_grad_clip(plan, float(scale), float(max_norm), *p, nbytes, _keep_table(plan, _stream(stream)))
+    _check(st, where)
     return st
 
 

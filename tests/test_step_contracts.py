@@ -114,7 +114,7 @@ p = C.comera_grad_plan((C.comera_grad_tensor * 1)((at[0], None, 100, C.BF16, 0))
 """
 
 
-def _without_torch(code):
+def _process(code):
     import os
     import subprocess
     import sys
@@ -125,4 +125,43 @@ def _without_torch(code):
 
 def test_addresses_without_torch():
     """Raw addresses and a stream need no torch."""
-    _without_torch(WITHOUT_TORCH)
+    _process(WITHOUT_TORCH)
+
+
+RAW_WORKSPACES = """
+from paper_2405_14377_amd import comera as C
+C.comera_debug_launch_check(True)
+at = [(1 << 40) + (i << 36) for i in range(40)]
+W = 1 << 34
+many = (C.comera_grad_tensor * 200)(*[(at[0] + 64 * i, None, 16, C.F32, 0) for i in range(200)])
+p = C.comera_grad_plan(many, 200)
+s, n = C.dense_embed_shape(100, 8), C.block_norm_shape(64, pre=C.NORM_RMS)
+
+
+def calls(ws, table):
+    yield lambda: C.comera_dense_embed_backward(s, at[0], 4, at[1], 1.0, -1, at[2], ws, stream=0)
+    yield lambda: C.comera_block_norm_backward(n, 4, at[0], None, None, None, None, at[1], at[2], at[3], at[4], None,
+                                               None, None, None, at[5], None, ws, stream=0)
+    yield lambda: C.comera_grad_plan_set_table(p, table, stream=0)
+    yield lambda: C.comera_grad_norm(p, 1.0, at[1], None, ws, stream=0)
+    yield lambda: C.comera_grad_clip(p, 1.0, 1.0, at[1], None, ws, stream=0)
+
+
+for call in calls((at[6], W), (at[7], C.comera_grad_table_bytes(p))):
+    assert call() == C.OK
+# too short, none, and an address without its bytes
+for ws in ((at[6], 8), None, at[6]):
+    for i, call in enumerate(calls(ws, ws)):
+        try:
+            call()
+        except C.ComeraError as e:
+            assert e.status == C.ERR_WORKSPACE, e
+        else:
+            assert ws is None and i == 2          # no table: allowed
+"""
+
+
+def test_raw_workspaces():
+    """A workspace or a table at a raw address comes with its bytes, with torch or without."""
+    _process(RAW_WORKSPACES)
+    _process("import sys\nsys.modules['torch'] = None\n" + RAW_WORKSPACES)
