@@ -291,8 +291,6 @@ namespace {
 
 struct Range {
     uintptr_t begin, end;
-    int64_t tensor;
-    bool written;
 };
 
 comera_status grad_args(comera_grad_plan_t p, float scale, const void *ws, size_t ws_bytes) {
@@ -346,8 +344,8 @@ comera_status comera_grad_plan(const comera_grad_tensor *tensors, int64_t count,
             const uintptr_t esz = t.dtype == COMERA_F32 ? 4 : 2, bytes = uintptr_t(t.n) * esz;
             const uintptr_t g = reinterpret_cast<uintptr_t>(t.g), o = reinterpret_cast<uintptr_t>(t.out);
             if (g % esz || o % esz) return COMERA_ERR_INVALID_ARG;
-            ranges.push_back({g, g + bytes, i, !o || o == g});
-            if (o && o != g) ranges.push_back({o, o + bytes, i, true});
+            ranges.push_back({g, g + bytes});
+            if (o && o != g) ranges.push_back({o, o + bytes});
             tiles += double((t.n + kTile - 1) / kTile);
             order.push_back(i);
             bytes_in += double(bytes);
