@@ -627,7 +627,10 @@ Spread narrow_spread(int N, int waves) {
 }
 
 // Forward: 8 entries a lane up to 512 columns; above, 12 or 16, whichever
-// leaves fewer idle lanes (768 columns: 64 lanes x 12).
+// leaves fewer idle lanes (768 columns: 64 lanes x 12).  RMS, 24 M entries,
+// with 12 and with 16: 768 columns bf16 41.0 and 42.9 us, fp32 73.3 and 74.9;
+// 1001 59.5 and 41.2, 78.6 and 75.3; 2304 41.0 and 42.4, 72.1 and 77.8; 4096
+// 64.9 and 38.5, 80.9 and 74.5.
 Spread fwd_spread(int N) {
     if (N <= 256) return narrow_spread(N, kWaveRows);
     if (N <= 512) return {8, 1, 64, kWaveRows};
@@ -651,10 +654,15 @@ Spread bwd_spread(int N) {
 }
 
 // One workgroup that takes up to two turns forms the parameters' gradients
-// itself: a call on 8 rows of 768 columns with bf16 RMS 13.9 -> 11.0 us, on 16
-// 13.8 -> 11.0, on 16 with LAYER 14.4 -> 15.0; four turns: on 32 12.8, with
-// LAYER 22.5.  Not above 4096 columns: one row of 8192 13.6 -> 14.9, with
-// LAYER 14.4 -> 20.1.
+// itself and saves a launch.  One launch and two, us a call in a row of calls,
+// which the host's launches bound, and the kernels alone (a replayed graph),
+// fp32: 8 rows of 768 columns RMS 8.1 and 10.5, kernels 5.9 and 7.6, LAYER 8.5
+// and 10.9, 7.1 and 8.9; 16 rows LAYER 9.3 and 10.8, 9.0 and 9.1.  The second
+// turn of wide rows costs the kernels alone more than a launch (two rows of
+// 4096 LAYER 9.6 and 10.7, 9.3 and 7.3), four turns cost more in any case (32
+// rows of 768 RMS 11.7 and 11.3, 11.2 and 7.7; LAYER 13.4 and 11.5, 13.2 and
+// 9.1).  Not above 4096 columns: one row of 8192 14.9 and 13.6, with LAYER
+// 20.1 and 14.4.
 bool bwd_alone(const Spread &sp, int N, int64_t b) { return b > 0 && b <= 2 * sp.rows && N <= 4096; }
 
 int64_t bwd_parts(const Spread &sp, int N, int64_t b) {

@@ -3,8 +3,9 @@
 //   backward  dT[v, :] = scale * sum over { t : ids[t] = v, v != pad } dY[t, :]
 // The forward copies rows: it is bound by the HBM bytes of its rows.  The
 // backward groups the tokens by id first (no floating-point atomics: every
-// row is summed in token order in fp32 and rounded once), then writes every
-// row of dT, the rows without tokens as zeros.
+// row is summed in fp32 in a fixed order and rounded once: token by token, or
+// where an id has many tokens in partial sums over runs of them that are added
+// in order), then writes every row of dT, the rows without tokens as zeros.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -613,7 +614,12 @@ __global__ __launch_bounds__(64 * kFinishWaves) void dense_finish_kernel(SumArgs
 // workgroup: 16384 Zipf ids 39.0 us in one part, 40.5 in two launches; 32768:
 // 51.2 and 50.0; 131072: 132 and 92 (table of 32768 x 768)
 constexpr int64_t kSplitTokens = 24576;
-// From here on chunks of 32 places instead of 16
+// From here on chunks of 32 places instead of 16: fewer partial rows, where
+// there are waves enough.  16 and 32 places, a table of 32768 x 768: 16384
+// uniform ids in fp32 44.2 and 47.0 us, in bf16 22.1 and 22.9 (Zipf ids 52.9
+// and 53.4, 30.5 and 28.2); 65536 uniform 82.6 and 83.0, 52.1 and 51.6 (Zipf
+// 99.9 and 93.6, 68.1 and 60.9); 131072 of a 5000 x 128 fp32 table 56.7 and
+// 36.1.  Between 24576 and here 32 would be level or up to 9 % faster.
 constexpr int64_t kLongChunks = 32768;
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
@@ -667,7 +673,6 @@ void dense_layout(const comera_dense_embed_shape *s, int64_t n, DenseLayout_ &L)
     const bool split = n >= (s->V > 4 ? kSplitTokens : kSplitTokens / 2);
     L.parts = split ? int(std::min<int64_t>(32, std::max<int64_t>(1, 256 / std::min(L.groups(), s->V)))) : 1;
     L.Q = int((s->V - 1) >> L.lg) + 1;
-    // longer chunks leave fewer partial rows, shorter ones more waves
     L.lgC = n < kLongChunks ? 4 : 5;
     // an id that begins at a chunk's last place ends within the 64 lanes
     L.few = std::min(64 - (1 << L.lgC), 1 << L.lgC);
