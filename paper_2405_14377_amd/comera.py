@@ -616,8 +616,9 @@ def comera_grad_clip(plan, scale: float, max_norm: float, norm, flag, ws, stream
 class GradPlan:
     """Owns the plan of a list of gradient tensors and a long list's table,
     and keeps the tensors alive.  outs: where the clipped gradients go (None,
-    or a None entry: in place).  Made outside a graph capture: a table is
-    waited for, so that calls on any stream find it.
+    or a None entry: in place).  Made once, for gradients that keep their
+    buffers: 361 tensors take 0.5 to 0.6 ms of the host.  Made outside a graph
+    capture: a table is waited for, so that calls on any stream find it.
 
     The plan may be dropped while calls through this module are pending: its
     table is kept until they are done (streams of one's own have to exist until
