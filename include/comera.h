@@ -476,10 +476,10 @@ void comera_grad_plan_destroy(comera_grad_plan_t p);
  * it, and the memory stays the plan's until the plan is destroyed or another
  * table (or NULL: none) is set, and the calls made until then have run; a
  * captured call reads it in every replay.  Not concurrently with other calls
- * on the same plan.  A short or misaligned (8 bytes) table -> WORKSPACE, a stream that is
- * being captured -> INVALID_ARG (the table would be written by the graph's
- * replays alone), and the plan is without one.  A table set in launch check
- * mode, which writes nothing, is used by calls in that mode only. */
+ * on the same plan.  A short or misaligned (8 bytes) table -> WORKSPACE, a
+ * stream that is being captured -> INVALID_ARG (the table would be written by
+ * the graph's replays alone), and the plan is without one.  A table set in
+ * launch check mode, which writes nothing, is used by calls in that mode only. */
 size_t comera_grad_table_bytes(comera_grad_plan_t p);
 comera_status comera_grad_plan_set_table(comera_grad_plan_t p, void *table, size_t bytes, void *stream);
 
